@@ -359,6 +359,110 @@ essa_status essa_cma_refresh_basis(essa_ctx* ctx, essa_cma* cma, int max_sweeps,
 /* The ranking alone.  rewards DEVICE float [K] -> order DEVICE int32 [K]; 1 <= K <= 1024. */
 essa_status essa_rank_rewards(essa_ctx* ctx, const float* rewards, int K, int32_t* order);
 
+/* ---------------------------------------------------------------------------------------------
+ * Key/value cache in 4 bits, and the attention that reads it  (what stands between a layer's q, k, v and its o
+ * projection while a candidate generates; paper: Algorithm 1, the inference pass of a candidate)
+ *
+ * A cache holds the keys and values of up to max_seqs sequences in pages of page_tokens tokens, one page for all layers.
+ * The caller owns the four DEVICE arrays of the descriptor and may read them at any time (in stream order); the calls
+ * below keep them:
+ *   pool   essa_kv_pool_bytes() bytes, 16-byte aligned: [n_pages][layers][n_kv_heads][page_tokens / 32] blocks of
+ *          36 head_dim bytes.  What a block looks like inside is the library's own; essa_kv_read gives its values.
+ *   table  int32 [max_seqs, max_pages]: the pages of a sequence in order, -1 past the last one
+ *   len    int32 [max_seqs]: tokens of a sequence
+ *   refs   int32 [n_pages]: how many sequences hold a page; 0 = free
+ * A full page may be held by several sequences; the partly filled last page of a sequence is always its own.
+ * Free pages are handed out lowest index first, so that equal calls give equal tables.  An entry of table or len that
+ * somebody else spoiled is brought into range before it is used.
+ *
+ * Format.  A group is 64 channels of one token and head.  With x clamped to +-2^15, lo and hi the least and the greatest
+ * of a group, and every operation rounded to nearest even in single precision:
+ *   s = fp16((hi - lo) / 15),  m = fp16(lo + 8 s),  q = min(max(rint((x - m) * (1 / s)), -8), 7)  (0 where s = 0)
+ * and the cache holds m + s q: 4.5 bits a value.  A group that holds an Inf or a NaN is held as 64 NaN.
+ * ------------------------------------------------------------------------------------------- */
+#define ESSA_KV_GROUP 64
+#define ESSA_KV_BLOCK 32
+typedef struct essa_kv essa_kv;
+typedef struct essa_kv_desc {
+    int32_t layers;      /* 1 .. 1024                                                                  */
+    int32_t n_kv_heads;  /* 1 .. 1024                                                                  */
+    int32_t head_dim;    /* 64 or 128                                                                  */
+    int32_t page_tokens; /* 32, 64, 128, 256, 512 or 1024                                              */
+    int32_t n_pages;     /* 1 .. 2^18                                                                  */
+    int32_t max_seqs;    /* 1 .. 4096                                                                  */
+    int32_t max_pages;   /* pages a sequence can have: max_pages * page_tokens < 2^31                  */
+    void* pool;
+    int32_t* table;
+    int32_t* len;
+    int32_t* refs;
+} essa_kv_desc;
+/* Bytes of the pool of a descriptor (its pointers are not looked at); 0 if its sizes are not valid. */
+size_t essa_kv_pool_bytes(const essa_kv_desc* desc);
+/* Makes an empty cache: table, len and refs are set (queued on the context's stream), the pool is left as it is. */
+essa_status essa_kv_create(essa_ctx* ctx, const essa_kv_desc* desc, essa_kv** out);
+void essa_kv_destroy(essa_kv* kv);
+
+/* Which rows of a call belong to which sequence.  n entries; entry b is sequence seqs[b] and owns rows
+ * row_start[b] .. row_start[b + 1] - 1 of the R rows, which are the LAST ones of the sequence: row j of its c rows is the
+ * token at position len - c + j.  row_start = NULL: one row an entry (R = n).  A negative seqs[b] is skipped, so the
+ * `served` of a call below can be passed on as it is; so is one past max_seqs.  The sequences of a call are distinct and
+ * row_start ascends from 0 to R (trusted; entries out of [0, R] are brought into it). */
+typedef struct essa_kv_batch {
+    const int32_t* seqs;      /* DEVICE int32 [n]             */
+    const int32_t* row_start; /* DEVICE int32 [n + 1] or NULL */
+    int32_t n;                /* 0 .. max_seqs                */
+    int32_t R;                /* 0 .. 2^24                    */
+} essa_kv_batch;
+
+/* What `served` says of an entry that was not served (negative, so that batches skip it). */
+#define ESSA_KV_SKIPPED (-1)  /* the entry was negative                                                */
+#define ESSA_KV_NO_PAGES (-2) /* no free pages left for it; the sequence is as it was                  */
+#define ESSA_KV_TOO_LONG (-3) /* it would have more than max_pages pages; the sequence is as it was    */
+#define ESSA_KV_BAD_ENTRY (-4)/* a sequence past max_seqs, one named twice (from the second on), a negative length */
+
+/* Lengthens sequence seqs[i] by n_new[i] tokens and gives it the pages that they need (a step's first call; the new
+ * tokens' keys and values are put in by essa_kv_append, layer by layer).  Entries are served in order; once the free
+ * pages do not suffice for one, no later entry of the call gets new pages.
+ *   seqs, n_new DEVICE int32 [n]    served DEVICE int32 [n] or NULL: seqs[i], or why not */
+essa_status essa_kv_extend(essa_ctx* ctx, essa_kv* kv, const int32_t* seqs, const int32_t* n_new, int n, int32_t* served);
+
+/* dst[i] becomes the first min(len[i], length of src[i]) tokens of src[i] as it was before the call, for all entries at
+ * once (so a permutation of sequences is one call); its own pages go back.  Full pages are shared, the partly filled last
+ * one is copied in every layer (the blocks of 32 tokens that hold kept tokens).  src[i] = dst[i] cuts a sequence in place;
+ * a page that the cut leaves partly filled is copied if another sequence holds it or another entry of the call forks from
+ * this one.  A negative src[i] frees dst[i].  Pages that the call gives back are not handed out by the same call.
+ *   src, dst DEVICE int32 [n]    len DEVICE int32 [n] or NULL = whole (so is a negative entry)
+ *   served   DEVICE int32 [n] or NULL: dst[i], or why not */
+essa_status essa_kv_fork(essa_ctx* ctx, essa_kv* kv, const int32_t* src, const int32_t* dst, const int32_t* len, int n, int32_t* served);
+/* Frees sequences: essa_kv_fork with every src negative. */
+essa_status essa_kv_free(essa_ctx* ctx, essa_kv* kv, const int32_t* seqs, int n);
+/* Moves the pages in use into pages 0 .. used - 1: those at or above `used` go, in ascending order, to the free ones
+ * below it; table and refs follow.
+ *   map_out  DEVICE int32 [n_pages] or NULL: a page's new index, -1 for a free one    used_out DEVICE int32 [1] or NULL */
+essa_status essa_kv_compact(essa_ctx* ctx, essa_kv* kv, int32_t* map_out, int32_t* used_out);
+
+/* Puts the rows' keys and values of one layer into the pages of their sequences, in 4 bits.  Every page of a row must be
+ * the sequence's own: rows that essa_kv_extend made room for are.
+ *   K, V  DEVICE [R] rows of n_kv_heads * head_dim values of x_dtype, row i at k_stride * i, v_stride * i (in values) */
+essa_status essa_kv_append(essa_ctx* ctx, essa_kv* kv, int layer, const void* K, int64_t k_stride, const void* V, int64_t v_stride, int x_dtype,
+                           const essa_kv_batch* batch);
+/* The values that the cache holds for the rows (zeros for rows without a token: skipped entries, positions below 0). */
+essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, int64_t k_stride, void* V, int64_t v_stride, int y_dtype,
+                         const essa_kv_batch* batch);
+
+/* Attention of the rows over the cached tokens of their sequences, one layer:
+ *   Y[i, h, :] = sum_t p_t V[t, h / g, :],  p = softmax over the tokens t that row i sees of  scale * < Q[i, h, :], K[t, h / g, :] >,
+ * g = n_q_heads / n_kv_heads, K and V what the cache holds.  The row at position p sees the tokens 0 .. p (its own is in
+ * the cache: append first), with window > 0 only the last `window` of them, with ESSA_KV_ALL (and window = 0) every token
+ * of the sequence.  A row that sees no token gives zeros.  What the row does not see has no part in it, NaN or not; a row
+ * of Q that holds an Inf or a NaN gives a row of NaN, a NaN in a K or V that it sees a NaN in that head.
+ *   Q  DEVICE [R] rows of n_q_heads * head_dim values of x_dtype at q_stride * i;  Y likewise, y_dtype, y_stride
+ * Arithmetic: bf16 Q -> products on the fp16 MFMA with fp32 accumulation, softmax statistics in fp32; fp32 Q -> fp32
+ * throughout. */
+#define ESSA_KV_ALL 0x1u
+essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
+                              const essa_kv_batch* batch, float scale, int window, uint32_t flags, void* Y, int64_t y_stride, int y_dtype);
+
 #ifdef __cplusplus
 }
 #endif

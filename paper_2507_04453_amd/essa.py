@@ -17,6 +17,8 @@ __all__ = [
     "ForwardGroup", "REWARD_BLOCK", "essa_svdlora_forward_reward_group", "essa_reward_finish",
     "essa_cma_create_opt", "OPT_CMA", "OPT_ACTIVE_CMA", "OPT_SEP_CMA", "OPT_ES", "OPT_ARS",
     "VALIDATE", "essa_svdlora_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
+    "KvCache", "KvBatch", "essa_kv_create", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact", "essa_kv_append", "essa_kv_read",
+    "essa_kv_attention", "KV_GROUP", "KV_BLOCK", "KV_SKIPPED", "KV_NO_PAGES", "KV_TOO_LONG", "KV_BAD_ENTRY", "KV_ALL",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libessa.so")
@@ -27,6 +29,9 @@ COMPUTE_W8A8, LORA_ONLY, BASE_ONLY, COMPUTE_BF16, VALIDATE = 1, 2, 4, 8, 16
 NOALLOC_SCRATCH_BYTES = 8 << 20
 MAX_GROUP = 8
 REWARD_BLOCK = 128
+KV_GROUP, KV_BLOCK = 64, 32
+KV_SKIPPED, KV_NO_PAGES, KV_TOO_LONG, KV_BAD_ENTRY = -1, -2, -3, -4
+KV_ALL = 1
 OPT_CMA, OPT_ACTIVE_CMA, OPT_SEP_CMA, OPT_ES, OPT_ARS = 0, 1, 2, 3, 4
 
 EXPORTED_SYMBOLS = [
@@ -40,6 +45,8 @@ EXPORTED_SYMBOLS = [
     "essa_svdlora_forward_reward_group", "essa_reward_finish",
     "essa_graph_begin", "essa_graph_end", "essa_graph_launch", "essa_graph_destroy", "essa_cma_refresh_basis",
     "essa_cma_create_opt", "essa_cma_kind", "essa_svdlora_forward_noalloc",
+    "essa_kv_pool_bytes", "essa_kv_create", "essa_kv_destroy", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact",
+    "essa_kv_append", "essa_kv_read", "essa_kv_attention",
 ]
 
 
@@ -63,6 +70,15 @@ class _FwdItem(C.Structure):
     _fields_ = [("proj", C.c_void_p), ("X", C.c_void_p), ("row2cand", C.c_void_p), ("sigmaA", C.c_void_p),
                 ("sigmaB", C.c_void_p), ("Y", C.c_void_p), ("sigma_stride", C.c_int64), ("R", C.c_int32),
                 ("K", C.c_int32)]
+
+
+class _KvDesc(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int32),
+                ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("pool", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class _KvBatch(C.Structure):
+    _fields_ = [("seqs", C.c_void_p), ("row_start", C.c_void_p), ("n", C.c_int32), ("R", C.c_int32)]
 
 
 def _load():
@@ -107,6 +123,16 @@ def _load():
         "essa_reward_accumulate_group": (i32, [vp, i32, C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), i32, i32, vp, i32, vp]),
         "essa_cmaes_update": (i32, [vp, vp, vp, vp, i32, vp]),
         "essa_rank_rewards": (i32, [vp, vp, i32, vp]),
+        "essa_kv_pool_bytes": (C.c_size_t, [C.POINTER(_KvDesc)]),
+        "essa_kv_create": (i32, [vp, C.POINTER(_KvDesc), C.POINTER(vp)]),
+        "essa_kv_destroy": (None, [vp]),
+        "essa_kv_extend": (i32, [vp, vp, vp, vp, i32, vp]),
+        "essa_kv_fork": (i32, [vp, vp, vp, vp, vp, i32, vp]),
+        "essa_kv_free": (i32, [vp, vp, vp, i32]),
+        "essa_kv_compact": (i32, [vp, vp, vp, vp]),
+        "essa_kv_append": (i32, [vp, vp, i32, vp, i64, vp, i64, i32, C.POINTER(_KvBatch)]),
+        "essa_kv_read": (i32, [vp, vp, i32, vp, i64, vp, i64, i32, C.POINTER(_KvBatch)]),
+        "essa_kv_attention": (i32, [vp, vp, i32, vp, i64, i32, i32, C.POINTER(_KvBatch), f32, i32, u32, vp, i64, i32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -546,3 +572,127 @@ def essa_rank_rewards(ctx: Context, rewards: torch.Tensor, order: torch.Tensor):
     if order.numel() != K:
         raise ValueError("order must hold K entries")
     _check(lib.essa_rank_rewards(ctx._h, _dev(rewards, torch.float32, "rewards"), K, _dev(order, torch.int32, "order")))
+
+
+class KvCache:
+    """essa_kv: keys and values of up to max_seqs sequences in 4 bits, in pages of page_tokens tokens (every layer of them).
+
+    The arrays are this object's tensors and may be read at any time (in stream order): pool (uint8 [n_pages, layers,
+    n_kv_heads, page_tokens / 32, 36 head_dim]), table (int32 [max_seqs, max_pages], -1 past a sequence's last page),
+    len (int32 [max_seqs]) and refs (int32 [n_pages], 0 = free)."""
+
+    def __init__(self, ctx: Context, layers: int, n_kv_heads: int, head_dim: int, n_pages: int, page_tokens: int = 64, max_seqs: int = 256,
+                 max_tokens: int = 4096):
+        self.ctx, self.layers, self.n_kv_heads, self.head_dim = ctx, layers, n_kv_heads, head_dim
+        self.n_pages, self.page_tokens, self.max_seqs = n_pages, page_tokens, max_seqs
+        self.max_pages = -(-max_tokens // page_tokens) if page_tokens > 0 else 0
+        self._h = C.c_void_p()
+        d = _KvDesc(layers, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, self.max_pages, None, None, None, None)
+        if lib.essa_kv_pool_bytes(C.byref(d)):
+            dev = torch.device("cuda", ctx.device)
+            self.pool = torch.empty(n_pages, layers, n_kv_heads, page_tokens // KV_BLOCK, 36 * head_dim, dtype=torch.uint8, device=dev)
+            self.table = torch.empty(max_seqs, self.max_pages, dtype=torch.int32, device=dev)
+            self.len = torch.empty(max_seqs, dtype=torch.int32, device=dev)
+            self.refs = torch.empty(n_pages, dtype=torch.int32, device=dev)
+            d.pool, d.table, d.len, d.refs = self.pool.data_ptr(), self.table.data_ptr(), self.len.data_ptr(), self.refs.data_ptr()
+        _check(lib.essa_kv_create(ctx._h, C.byref(d), C.byref(self._h)))       # invalid sizes are refused there
+
+    def close(self):
+        if self._h:
+            lib.essa_kv_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def essa_kv_create(ctx, layers, n_kv_heads, head_dim, n_pages, page_tokens=64, max_seqs=256, max_tokens=4096) -> KvCache:
+    return KvCache(ctx, layers, n_kv_heads, head_dim, n_pages, page_tokens, max_seqs, max_tokens)
+
+
+class KvBatch:
+    """Which rows of a call belong to which sequence: entry b is sequence seqs[b] (int32 [n], negative = skipped) and owns rows
+    row_start[b] .. row_start[b + 1] - 1 of R (int32 [n + 1]; None: one row an entry), the last ones of its sequence.  Marshalled
+    once; holds the tensors, whose contents may change from call to call."""
+
+    def __init__(self, seqs: torch.Tensor, row_start: "torch.Tensor | None" = None, R: "int | None" = None):
+        n = seqs.numel()
+        if row_start is None:
+            if R is not None and R != n:
+                raise ValueError("without row_start there is one row an entry")
+            R = n
+        elif R is None or row_start.numel() != n + 1:
+            raise ValueError("row_start must be [n + 1], with R given")
+        self.n, self.R, self._keep = n, R, (seqs, row_start)
+        self.arg = _KvBatch(_dev(seqs, torch.int32, "seqs"), _dev(row_start, torch.int32, "row_start"), n, R)
+        self.ref = C.byref(self.arg)
+
+
+def _entries(kv, name, t, n):
+    if t is not None and t.numel() != n:
+        raise ValueError("%s must hold one entry for each of the %d sequences" % (name, n))
+    return _dev(t, torch.int32, name)
+
+
+def essa_kv_extend(ctx: Context, kv: KvCache, seqs: torch.Tensor, n_new: torch.Tensor, served: torch.Tensor | None = None):
+    n = seqs.numel()
+    _check(lib.essa_kv_extend(ctx._h, kv._h, _entries(kv, "seqs", seqs, n), _entries(kv, "n_new", n_new, n), n, _entries(kv, "served", served, n)))
+
+
+def essa_kv_fork(ctx: Context, kv: KvCache, src: torch.Tensor, dst: torch.Tensor, lens: torch.Tensor | None = None, served: torch.Tensor | None = None):
+    n = dst.numel()
+    _check(lib.essa_kv_fork(ctx._h, kv._h, _entries(kv, "src", src, n), _entries(kv, "dst", dst, n), _entries(kv, "lens", lens, n), n,
+                            _entries(kv, "served", served, n)))
+
+
+def essa_kv_free(ctx: Context, kv: KvCache, seqs: torch.Tensor):
+    n = seqs.numel()
+    _check(lib.essa_kv_free(ctx._h, kv._h, _entries(kv, "seqs", seqs, n), n))
+
+
+def essa_kv_compact(ctx: Context, kv: KvCache, map_out: torch.Tensor | None = None, used_out: torch.Tensor | None = None):
+    if (map_out is not None and map_out.numel() != kv.n_pages) or (used_out is not None and used_out.numel() != 1):
+        raise ValueError("map_out must be [n_pages], used_out [1]")
+    _check(lib.essa_kv_compact(ctx._h, kv._h, _dev(map_out, torch.int32, "map_out"), _dev(used_out, torch.int32, "used_out")))
+
+
+def _kv_rows(t, R, heads, D, name):
+    """Pointer and row stride (in values) of [R, heads, D] or [R, heads * D] rows; the rows themselves are dense, their distance is free."""
+    if t.dim() == 3:
+        dense = t.shape[1] == heads and t.shape[2] == D and t.stride(2) == 1 and (heads == 1 or t.stride(1) == D)
+    else:
+        dense = t.dim() == 2 and t.shape[1] == heads * D and t.stride(1) == 1
+    if not (dense or t.numel() == 0) or t.shape[0] != R:
+        raise ValueError("%s must be [%d, %d, %d] (or its last two dimensions in one) with dense rows" % (name, R, heads, D))
+    if not t.is_cuda:
+        raise TypeError("%s must be a torch tensor on the GPU" % name)
+    return t.data_ptr(), t.stride(0) if R > 1 else heads * D
+
+
+def essa_kv_append(ctx: Context, kv: KvCache, layer: int, K: torch.Tensor, V: torch.Tensor, batch: KvBatch):
+    if K.dtype != V.dtype:
+        raise TypeError("K and V share a dtype")
+    k, ks = _kv_rows(K, batch.R, kv.n_kv_heads, kv.head_dim, "K")
+    v, vs = _kv_rows(V, batch.R, kv.n_kv_heads, kv.head_dim, "V")
+    _check(lib.essa_kv_append(ctx._h, kv._h, layer, k, ks, v, vs, _xdtype(K), batch.ref))
+
+
+def essa_kv_read(ctx: Context, kv: KvCache, layer: int, K: torch.Tensor, V: torch.Tensor, batch: KvBatch):
+    """K, V: outputs, [R, n_kv_heads, head_dim]."""
+    if K.dtype != V.dtype:
+        raise TypeError("K and V share a dtype")
+    k, ks = _kv_rows(K, batch.R, kv.n_kv_heads, kv.head_dim, "K")
+    v, vs = _kv_rows(V, batch.R, kv.n_kv_heads, kv.head_dim, "V")
+    _check(lib.essa_kv_read(ctx._h, kv._h, layer, k, ks, v, vs, _ydtype(K), batch.ref))
+
+
+def essa_kv_attention(ctx: Context, kv: KvCache, layer: int, Q: torch.Tensor, Y: torch.Tensor, batch: KvBatch, scale: float, window: int = 0,
+                      causal: bool = True):
+    """Q, Y: [R, n_q_heads, head_dim] (or [R, n_q_heads * head_dim]); window 0: none."""
+    heads = Q.shape[1] if Q.dim() == 3 else Q.shape[-1] // kv.head_dim
+    q, qs = _kv_rows(Q, batch.R, heads, kv.head_dim, "Q")
+    y, ys = _kv_rows(Y, batch.R, heads, kv.head_dim, "Y")
+    _check(lib.essa_kv_attention(ctx._h, kv._h, layer, q, qs, _xdtype(Q), heads, batch.ref, scale, window, 0 if causal else KV_ALL, y, ys, _ydtype(Y)))
