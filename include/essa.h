@@ -376,8 +376,8 @@ essa_status essa_rank_rewards(essa_ctx* ctx, const float* rewards, int K, int32_
  * somebody else spoiled is brought into range before it is used.
  *
  * Format.  A group is 64 channels of one token and head.  With x clamped to +-2^15, lo and hi the least and the greatest
- * of a group, and every operation rounded to nearest even in single precision:
- *   s = fp16((hi - lo) / 15),  m = fp16(lo + 8 s),  q = min(max(rint((x - m) * (1 / s)), -8), 7)  (0 where s = 0)
+ * of a group, r = 1 / 15 in single precision, and every operation rounded to nearest even in single precision:
+ *   s = fp16((hi - lo) * r),  m = fp16(lo + 8 s),  q = min(max(rint((x - m) * (1 / s)), -8), 7)  (0 where s = 0)
  * and the cache holds m + s q: 4.5 bits a value.  A group that holds an Inf or a NaN is held as 64 NaN.
  * ------------------------------------------------------------------------------------------- */
 #define ESSA_KV_GROUP 64

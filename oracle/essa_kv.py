@@ -15,7 +15,7 @@ def kv_quantise(x):
     finite = np.isfinite(g).all(-1)
     g = np.clip(np.where(np.isfinite(g), g, np.float32(0)), np.float32(-32768), np.float32(32768))
     lo, hi = g.min(-1), g.max(-1)
-    s = ((hi - lo) / np.float32(15)).astype(np.float16).astype(np.float32)
+    s = ((hi - lo) * (np.float32(1) / np.float32(15))).astype(np.float16).astype(np.float32)
     m = (lo + np.float32(8) * s).astype(np.float16).astype(np.float32)
     inverse = np.where(s > 0, np.float32(1) / np.where(s > 0, s, np.float32(1)), np.float32(0)).astype(np.float32)
     q = np.clip(np.rint((g - m[..., None]) * inverse[..., None]), -8, 7)

@@ -5,6 +5,13 @@
 
 namespace {
 
+// The compiler makes one instruction of a product or sum and its conversion (v_fma_mixlo_f16), which rounds once; the format
+// rounds to single precision first.
+__device__ __forceinline__ __half half_of_single(float x) {
+    asm volatile("" : "+v"(x));
+    return __float2half_rn(x);
+}
+
 // A workgroup takes the new tokens of one block and one head: eight threads a token, D / 8 channels each, so that a group
 // of 64 channels is 4 (D = 128) or 8 (D = 64) neighbouring lanes.  Keys go out as each thread has them (its channels are
 // whole words of its token); the words of values hold one channel of eight tokens and are put together through LDS, those
@@ -49,9 +56,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, 
             hi = fmaxf(hi, __shfl_xor(hi, m));
             finite &= (bool)__shfl_xor((int)finite, m);
         }
-        const __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+        const __half sh = half_of_single(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f));
         const float s = __half2float(sh);
-        const __half mh = __float2half_rn(__fadd_rn(lo, 8.f * s));
+        const __half mh = half_of_single(__fadd_rn(lo, 8.f * s));
         const float m = __half2float(mh), inverse = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
         uint32_t word[CH / 8];
 #pragma unroll
