@@ -79,10 +79,11 @@ __device__ int entry_sums(int* prefix, int n, int* waves) {
     return total;
 }
 
-__global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len, int max_seqs, int32_t* refs, int n_pages) {
+__global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len, int max_seqs, int32_t* refs, int n_pages, int32_t* done) {
     const long long step = (long long)gridDim.x * blockDim.x;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < entries; i += step) table[i] = -1;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < max_seqs; i += step) len[i] = 0;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < 2 * essa_k::kKvAttnWorkgroups; i += step) done[i] = 0;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_pages; i += step) refs[i] = 0;
 }
 
@@ -315,7 +316,7 @@ pages_view view_of(const essa_kv* kv) {
 namespace essa_k {
 
 size_t kv_scratch_words(const essa_kv_desc& d) {
-    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4;
+    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4 + 2 * kKvAttnWorkgroups;
 }
 kv_scratch kv_scratch_of(const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
@@ -326,13 +327,14 @@ kv_scratch kv_scratch_of(const essa_kv* kv) {
     s.entry_page = s.entry_len + d.max_seqs;
     s.entry_ok = s.entry_page + d.max_seqs;
     s.count = s.entry_ok + d.max_seqs;
-    s.rows = s.count + 4;
+    s.done = s.count + 4;
+    s.rows = s.done + 2 * kKvAttnWorkgroups;
     return s;
 }
 
 hipError_t kv_clear(hipStream_t st, const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
-    kv_clear_kernel<<<512, 256, 0, st>>>(d.table, (long long)d.max_seqs * d.max_pages, d.len, d.max_seqs, d.refs, d.n_pages);
+    kv_clear_kernel<<<512, 256, 0, st>>>(d.table, (long long)d.max_seqs * d.max_pages, d.len, d.max_seqs, d.refs, d.n_pages, kv_scratch_of(kv).done);
     return hipGetLastError();
 }
 

@@ -179,7 +179,7 @@ extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int l
     const char* who = "essa_kv_attention";
     ESSA_TRY(check_kv(ctx, kv, who));
     ESSA_TRY(check_rows(kv, layer, batch, who));
-    if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % kv->d.n_kv_heads)
+    if (n_q_heads < 1 || n_q_heads > 32768 || n_q_heads % kv->d.n_kv_heads)
         return essa_fail(ESSA_ERR_SHAPE, "%s: %d query heads on %d key heads", who, n_q_heads, kv->d.n_kv_heads);
     if (flags & ~ESSA_KV_ALL) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
     if (window < 0 || (window > 0 && (flags & ESSA_KV_ALL)))
@@ -195,6 +195,7 @@ extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int l
     const essa_k::kv_view v = view_of(kv, layer);
     const essa_k::kv_rows rows = rows_of(batch);
     ESSA_TRY(essa_ws_reserve(ctx, essa_k::kv_attention_bytes(v, kv->d.head_dim, n_q_heads, rows, x_dtype)));
-    ESSA_HIP(essa_k::kv_attention(ctx->stream, v, kv->d.head_dim, q, y, n_q_heads, rows, scale, window, (flags & ESSA_KV_ALL) != 0, ctx->ws));
+    ESSA_HIP(essa_k::kv_attention(ctx->stream, v, kv->d.head_dim, q, y, n_q_heads, rows, scale, window, (flags & ESSA_KV_ALL) != 0,
+                                  essa_k::kv_scratch_of(kv).done, ctx->ws));
     return ESSA_OK;
 }

@@ -47,12 +47,15 @@ struct kv_tensor {             // R rows of heads * D values
     int aligned;               // rows begin on 16 bytes
 };
 
-// scratch of the bookkeeping (int32 words)
+constexpr int kKvAttnWorkgroups = 768;     // three a CU
+
+// the cache's scratch (int32 words): page bookkeeping, and attention's counts
 struct kv_scratch {
     int32_t *list, *map;       // [n_pages] each
     int32_t *entry_len, *entry_page, *entry_ok;   // [max_seqs] each
     int32_t* rows;             // [max_seqs, max_pages]
     int32_t* count;            // [4]
+    int32_t* done;             // [2 kKvAttnWorkgroups] attention's counts of finished parts, 0 between calls
 };
 size_t kv_scratch_words(const essa_kv_desc& d);
 kv_scratch kv_scratch_of(const essa_kv* kv);
@@ -67,5 +70,5 @@ hipError_t kv_read(hipStream_t st, const kv_view& v, int D, const kv_tensor& K, 
 
 size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& rows, int x_dtype);
 hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale,
-                        int window, bool all, void* ws);
+                        int window, bool all, int32_t* done, void* ws);
 }  // namespace essa_k
