@@ -72,7 +72,17 @@ struct attn_args {
     int* done;                 // [2 workgroups] see join; 0 between calls
     float* parts;              // [2 workgroups][kColumns][D + 4]: sum of a column's weights, their largest exponent, -, -, weighted values
     int least;                 // what a workgroup takes at least
+    // prompts: tiles of kTile columns of an entry, one after another, and how far the units before a tile reach
+    int* tiles;                // [1] how many; null: this call has none
+    int* tile_at;              // [tiles + 1]
+    int2* tile;                // [tiles] entry, which of its tiles
+    int tile_grain, tile_least;
 };
+constexpr int kTile = 256, kStage = 64, kTileCost = 3;
+// An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16): there a
+// block is unpacked once for 256 columns instead of once for 16.  At 65 columns and 4000 tokens the two kernels are even.
+template <bool F32>
+__device__ __forceinline__ bool is_prompt(const attn_args& a, int rows) { return !F32 && a.tiles && rows > 1 && (long long)rows * a.g > kColumns; }
 
 struct entry_span {            // the blocks that an entry's rows see, and how many units of kColumns columns it has for each key head
     int lo, n, groups;
@@ -92,8 +102,9 @@ struct attn_list {
     int4* entry;               // [n] slot, len, row0, rows
     int even;                  // > 0: every unit counts as this long
 };
-inline size_t list_bytes(int n) { return (size_t)n * sizeof(int4) + ((size_t)n + 1) * sizeof(int); }
+inline size_t list_bytes(int n) { return (size_t)n * sizeof(int4) + ((size_t)n + 1) * 2 * sizeof(int); }      // and one int more an entry for planning tiles
 
+template <bool F32>
 __device__ attn_list make_list(const attn_args& a, void* lds) {                // 256 threads
     __shared__ int waves[3][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
@@ -102,7 +113,8 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     for (int b = lo; b < hi; ++b) {
         const kv_entry e = kv_entry_of(a.v, a.rows, b);
         const entry_span s = span_of(a, e.len, e.rows);
-        const int size = s.n ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = s.n ? s.groups * a.v.heads : 0;
+        const bool here = s.n && !is_prompt<F32>(a, e.rows);
+        const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.entry[b] = int4{e.slot, e.len, e.row0, e.rows};
         length += size * u;
         units += u;
@@ -133,7 +145,8 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     for (int b = lo; b < hi; ++b) {
         const int4 e = l.entry[b];
         const entry_span s = span_of(a, e.y, e.w);
-        const int size = s.n ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = s.n ? s.groups * a.v.heads : 0;
+        const bool here = s.n && !is_prompt<F32>(a, e.w);
+        const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.at[b] = l.even ? units_at * l.even : length_at;
         length_at += size * u;
         units_at += u;
@@ -154,20 +167,97 @@ __device__ __forceinline__ int entry_at(const attn_list& l, int n, int at) {
     return lo;
 }
 
+// ---------------------------------------------------------------------------------------------
+// Prompts' tiles: kTile consecutive columns of an entry, over the stages of kStage tokens that its rows see; a unit for each
+// key head.
+// ---------------------------------------------------------------------------------------------
+struct tile_span {
+    int lo, n, columns;        // first stage, stages, columns
+};
+__device__ __forceinline__ tile_span tile_of(const attn_args& a, int len, int rows, int which) {
+    tile_span t;
+    const int c0 = which * kTile;
+    t.columns = (int)min((long long)rows * a.g - c0, (long long)kTile);
+    const int first = len - rows + c0 / a.g, last = len - rows + (c0 + t.columns - 1) / a.g;      // positions
+    const int lo = a.window > 0 ? max(first - a.window + 1, 0) : 0, hi = a.all ? len : min(last + 1, len);
+    t.lo = lo / kStage;
+    t.n = max((hi + kStage - 1) / kStage - t.lo, 0);
+    return t;
+}
+// One workgroup of the stream kernel lists them for the prompt kernel behind it.
+__device__ void plan_tiles(const attn_args& a, const attn_list& l) {           // 256 threads
+    __shared__ int waves[4];
+    const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
+    int* first = l.at + n + 1;                                 // [n + 1] tiles in front of an entry
+    const auto add = [](int x, int y) { return x + y; };
+    const auto block_scan = [&](int x, int& total) {           // sum over the threads before this one
+        const int to = wave_scan(x, add);
+        lds_barrier();
+        if ((threadIdx.x & 63) == 63) waves[threadIdx.x / 64] = to;
+        lds_barrier();
+        int before = to - x;
+        total = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            before += w < (int)threadIdx.x / 64 ? waves[w] : 0;
+            total += waves[w];
+        }
+        return before;
+    };
+    const auto tiles_of = [&](int b) {
+        const int4 e = l.entry[b];
+        return is_prompt<false>(a, e.w) && span_of(a, e.y, e.w).n ? (int)(((long long)e.w * a.g + kTile - 1) / kTile) : 0;
+    };
+    int mine = 0, tiles;
+    for (int b = lo; b < hi; ++b) mine += tiles_of(b);
+    int at = block_scan(mine, tiles);
+    for (int b = lo; b < hi; ++b) {
+        first[b] = at;
+        at += tiles_of(b);
+    }
+    if (threadIdx.x == 0) {
+        first[n] = tiles;
+        *a.tiles = tiles;
+    }
+    lds_barrier();
+    int done = 0;
+    for (int base = 0; base < tiles; base += 256) {
+        const int i = base + (int)threadIdx.x;
+        int size = 0, b = 0, total;
+        if (i < tiles) {
+            for (int end = n; end - b > 1;) {
+                const int mid = (b + end) / 2;
+                if (first[mid] <= i) b = mid;
+                else end = mid;
+            }
+            const int4 e = l.entry[b];
+            const tile_span t = tile_of(a, e.y, e.w, i - first[b]);
+            size = (((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost) * a.v.heads;
+        }
+        const int before = done + block_scan(size, total);
+        if (i < tiles) {
+            a.tile[i] = int2{b, i - first[b]};
+            a.tile_at[i] = before;
+        }
+        done += total;
+    }
+    if (threadIdx.x == 0) a.tile_at[tiles] = done;
+}
+
 // Parts of units that other workgroups read: written through to where every XCD sees them, and read from there, eight bytes
 // at a time (slot: the workgroup's part of the unit that began before it, or of the one that goes on after it).
-template <int D>
-__device__ __forceinline__ void put_part(float* parts, int slot, int column, int c, const f32x4& y, float weight, float best) {
-    unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * kColumns + column) * (D + 4));
+template <int D, int COLUMNS>
+__device__ __forceinline__ void put_part(float* parts, long long slot, int column, int c, const f32x4& y, float weight, float best) {
+    unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
     typedef __attribute__((ext_vector_type(2))) float f32x2;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         __hip_atomic_store(p + 2 + c / 2 + i, __builtin_bit_cast(unsigned long long, f32x2{y[2 * i], y[2 * i + 1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (c == 0) __hip_atomic_store(p, __builtin_bit_cast(unsigned long long, f32x2{weight, best}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-template <int D>
-__device__ __forceinline__ void get_part(const float* parts, int slot, int column, int c, f32x4& y, float& weight, float& best) {
-    const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * kColumns + column) * (D + 4));
+template <int D, int COLUMNS>
+__device__ __forceinline__ void get_part(const float* parts, long long slot, int column, int c, f32x4& y, float& weight, float& best) {
+    const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     const f32x2 head = __builtin_bit_cast(f32x2, __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     weight = head[0];
@@ -191,6 +281,49 @@ __device__ __forceinline__ bool last_to_come(int* count, int others, int* last_o
     }
     __syncthreads();
     return *last_one;
+}
+
+// Parts w_first .. w_last of a unit, this workgroup's among them and written, become its result: in two steps, sixteen
+// consecutive ones and then the sixteens, so that a workgroup reads at most 16 + 48 of them.  A column's quads are neighbouring
+// lanes: all of them have read a part before one writes the sixteen's sum in its place.
+template <int D, int COLUMNS, int THREADS, class Finish>
+__device__ void join_parts(float* parts, int* done, int w_first, int w_last, int columns, int* last_one, Finish finish) {
+    constexpr int QUADS = D / 4;
+    const int group = ((int)blockIdx.x - w_first) >> 4, g_first = w_first + 16 * group, g_last = min(g_first + 15, w_last), groups = (w_last - w_first >> 4) + 1;
+    const auto join = [&](int from, int to, int step, bool final) {
+        for (int i = threadIdx.x; i < columns * QUADS; i += THREADS) {
+            const int col = i / QUADS, c = 4 * (i % QUADS);
+            float best = -kFar, weight = 0.f;
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+            for (int w = from; w <= to; w += 8 * step) {
+                f32x4 in[8];
+                float in_weight[8], in_best[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int ww = min(w + k * step, to);                      // those past the end are read twice and not used
+                    get_part<D, COLUMNS>(parts, 2 * (long long)ww + (ww == w_first), col, c, in[k], in_weight[k], in_best[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (w + k * step <= to) {
+                        const float now = fmaxf(best, in_best[k]);
+                        const float f = best == now ? 1.f : __builtin_amdgcn_exp2f(best - now), f2 = in_best[k] == now ? 1.f : __builtin_amdgcn_exp2f(in_best[k] - now);
+                        y = y * f + in[k] * f2;
+                        weight = weight * f + in_weight[k] * f2;
+                        best = now;
+                    }
+            }
+            if (final) finish(col, c, y, weight);
+            else put_part<D, COLUMNS>(parts, 2 * (long long)from + (from == w_first), col, c, y, weight, best);
+        }
+    };
+    if (g_last > g_first) {
+        if (!last_to_come(&done[2 * g_first], g_last - g_first, last_one)) return;
+        join(g_first, g_last, 1, groups == 1);
+    }
+    if (groups == 1) return;
+    if (!last_to_come(&done[2 * w_first + 1], groups - 1, last_one)) return;
+    join(w_first, w_first + 16 * (groups - 1), 16, true);
 }
 
 // eight values of a row as they are in memory
@@ -236,6 +369,7 @@ __device__ __forceinline__ void load_raw(const kv_tensor& Q, long long at, uint3
 // weights stay below 2^3 and times a scale (at most 4370) below the range of fp16.
 // ---------------------------------------------------------------------------------------------
 constexpr float kSlack = 2.f;  // what a score may pass the running maximum by, as an exponent of 2
+constexpr float kTileSlack = 8.f, kTileLift = 4.f;            // prompts: weights alone have to fit into fp16
 constexpr float kLift = 1.f;   // weights are 2^kLift larger than they have to be: fp16's small numbers reach further down
 
 template <int D>
@@ -534,7 +668,8 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
     row_of* merged = (row_of*)ring;                            // [4]: after a unit's last block
     static_assert(sizeof(row_of) * 4 <= sizeof ring, "");
     __shared__ int last_one;
-    const attn_list list = make_list(a, list_lds);
+    const attn_list list = make_list<F32>(a, list_lds);
+    if (a.tiles && blockIdx.x == gridDim.x - 1) plan_tiles(a, list);
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 4;
     const int total = uniform(list.at[a.rows.n]), part = list.even ? list.even : max(divide(total, (int)gridDim.x) + 1, a.least);
     const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
@@ -643,50 +778,14 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
                     weight += f * wsum[w][l];
                 }
             if (complete) finish(col, c, y, weight);
-            else put_part<D>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
+            else put_part<D, kColumns>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
         }
         if (complete) continue;
-        // Parts are joined in two steps, sixteen consecutive ones and then the sixteens: a workgroup reads at most 16 + 48 of them.
-        const int w_first = divide(unit_at + kUnitCost, part), w_last = divide(unit_at + size - 1, part);
-        const int group = ((int)blockIdx.x - w_first) >> 4, g_first = w_first + 16 * group, g_last = min(g_first + 15, w_last), groups = (w_last - w_first >> 4) + 1;
-        const auto join = [&](int from, int to, int step, bool final) {
-            for (int i = threadIdx.x; i < columns * QUADS; i += 256) {
-                const int col = i / QUADS, c = 4 * (i % QUADS);
-                float best = -kFar, weight = 0.f;
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                for (int w = from; w <= to; w += 8 * step) {
-                    f32x4 in[8];
-                    float in_weight[8], in_best[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int ww = min(w + k * step, to);                  // those past the end are read twice and not used
-                        get_part<D>(a.parts, 2 * ww + (ww == w_first), col, c, in[k], in_weight[k], in_best[k]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (w + k * step <= to) {
-                            const float now = fmaxf(best, in_best[k]);
-                            const float f = best == now ? 1.f : __builtin_amdgcn_exp2f(best - now), f2 = in_best[k] == now ? 1.f : __builtin_amdgcn_exp2f(in_best[k] - now);
-                            y = y * f + in[k] * f2;
-                            weight = weight * f + in_weight[k] * f2;
-                            best = now;
-                        }
-                }
-                if (final) finish(col, c, y, weight);
-                else put_part<D>(a.parts, 2 * from + (from == w_first), col, c, y, weight, best);
-            }
-        };
-        if (g_last > g_first) {
-            if (!last_to_come(&a.done[2 * g_first], g_last - g_first, &last_one)) continue;
-            join(g_first, g_last, 1, groups == 1);
-        }
-        if (groups == 1) continue;
-        if (!last_to_come(&a.done[2 * w_first + 1], groups - 1, &last_one)) continue;
-        join(w_first, w_first + 16 * (groups - 1), 16, true);
+        join_parts<D, kColumns, 256>(a.parts, a.done, divide(unit_at + kUnitCost, part), divide(unit_at + size - 1, part), columns, &last_one, finish);
     }
     // rows that see nothing: no unit holds them
     for (int b = blockIdx.x; b < a.rows.n; b += gridDim.x)
-        if (list.at[b] == list.at[b + 1]) {
+        if (list.at[b] == list.at[b + 1] && span_of(a, list.entry[b].y, list.entry[b].w).n == 0) {
             const int4 e = list.entry[b];
             const int width = a.g * a.v.heads * QUADS;
             for (int i = 0; i < e.w; ++i)
@@ -694,24 +793,372 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
         }
 }
 
+// ---------------------------------------------------------------------------------------------
+// Prompts: eight waves, 32 columns each, over stages of 64 tokens that all eight unpack together.
+//
+// Scores^T = K Q^T and O^T = V^T P^T on the 32 x 32 x 16 MFMA.  Keys and values stand in LDS as fp16 numbers m + s q: rounded
+// once more (2^-11 of themselves) than in the stream kernel, because scales on the scores would be four multiply-adds for
+// each of them and the vector ALU is what this kernel is short of: 16 scores of a lane cost some 110 issue slots against 16
+// MFMAs.  Rows of LDS are 16 bytes longer than their values: every 16 lanes that read together meet 64 different banks.
+// The tokens of a value's row stand in the order in which the first product leaves the scores.  While a stage is worked on
+// the next one is unpacked into the other buffer and the one after it is on its way from memory; one barrier a stage.
+// A NaN among the values must not reach columns that do not see it (0 times NaN): it is taken out and noted, and the
+// columns that see it get theirs at the end of the stage.
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+constexpr int kTileThreads = 512;
+
+template <int D>
+struct tile_lds {
+    static constexpr int KROW = 2 * D + 16, VROW = 2 * kStage + 16;            // bytes
+    unsigned char k[kStage * KROW];
+    unsigned char v[D * VROW];
+};
+
+// what a thread unpacks of a stage: D / 64 words of keys (consecutive ones of a lane's), as many of values
+template <int D>
+struct tile_words {
+    static constexpr int N = D / 64;
+    uint32_t k[N], v[N];
+    uint32_t k_scale;          // s in the low half, m in the high one
+    u32x4 v_s, v_m;
+};
+
+template <int D>
+__global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_args a) {
+    constexpr int N = D / 64, KK = D / 16, OT = D / 32, QUADS = D / 4, NG = D / kKvGroup, KROW = tile_lds<D>::KROW, VROW = tile_lds<D>::VROW;
+    __shared__ tile_lds<D> buffer[2];
+    __shared__ unsigned long long nans[3][NG];                 // tokens of a stage whose values are NaN, stage i's in i % 3
+    __shared__ int last_one;
+    const int tiles = uniform(*a.tiles);
+    if (tiles == 0) return;
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), l = lane & 31, hh = lane >> 5;
+    const int total = uniform(a.tile_at[tiles]), part = max(divide(total, (int)gridDim.x) + 1, a.tile_least);
+    const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
+    const int begin = part < 0x7fffffff / (int)gridDim.x ? blockIdx.x * part : (int)min((long long)blockIdx.x * part, 0x7fffffffll);
+    const int end = total - begin < part ? total : begin + part;
+    // where this thread's words lie in a block, and where they go in LDS
+    const int piece = threadIdx.x & 255, bk = wave >> 2, my_lane = N == 2 ? (piece & 127) >> 1 : piece >> 2;
+    const int k_word = N == 2 ? 4 * (piece >> 7) + 2 * (piece & 1) : piece & 3;                    // w of the layout: token tile and step of 32 channels
+    const int k_tok = 16 * (k_word / (D / 32)) + (my_lane & 15), k_chan = 32 * (k_word % (D / 32)) + 8 * (my_lane >> 4);
+    const int v_h = my_lane >> 4, v_chan = N == 2 ? 64 * (piece >> 7) + 32 * (piece & 1) + (my_lane & 15) : 16 * (piece & 3) + (my_lane & 15);
+    const int in_block = 1024 * (N == 2 ? piece >> 7 : 0) + 16 * my_lane + 4 * (N == 2 ? 2 * (piece & 1) : piece & 3);
+    const int k_scale_at = essa_k::kv_key_scales_at(D) + kv_scale_at(k_chan / kKvGroup, k_tok);
+    const int v_scale_at = essa_k::kv_value_scales_at(D) + (v_chan / kKvGroup * 4 + v_h) * 32;
+    const int k_to = (32 * bk + k_tok) * KROW + 2 * k_chan;
+    const int v_to = v_chan * VROW + 64 * bk + 16 * (v_h & 1) + 8 * (v_h >> 1);
+
+    for (int at = begin; at < end;) {
+        int ti = 0;
+        for (int hi = tiles; hi - ti > 1;) {
+            const int step = (hi - ti + 63) / 64, t = ti + lane * step;
+            const unsigned long long below = __ballot(t < hi && a.tile_at[min(t, tiles)] <= at) | 1;
+            ti += (63 - __builtin_clzll(below)) * step;
+            hi = min(hi, ti + step);
+        }
+        ti = uniform(ti);
+        const int b = uniform(a.tile[ti].x), which = uniform(a.tile[ti].y);
+        kv_entry e = kv_entry_of(a.v, a.rows, b);
+        const int slot = uniform(e.slot), len = uniform(e.len), row0 = uniform(e.row0), rows = uniform(e.rows);
+        const tile_span sp = tile_of(a, len, rows, which);
+        const int in = at - uniform(a.tile_at[ti]), grains = (sp.n + (1 << a.tile_grain) - 1) >> a.tile_grain, size = grains + kTileCost;
+        const int head = divide(in, size), unit_at = at - (in - head * size);
+        const int from = max(at - unit_at - kTileCost, 0), to = min(min(size, end - unit_at) - kTileCost, grains);
+        at = unit_at + size;
+        const bool begins = from == 0, complete = begins && to == grains;
+        if (grains > 0 && to <= from) continue;
+        if (grains == 0 && unit_at + kTileCost > end) continue;                // no row sees anything: whoever has all of its cost writes the zeros
+        const int first = sp.lo + (from << a.tile_grain), stop = sp.lo + min(to << a.tile_grain, sp.n);
+        const int columns = sp.columns, c0 = which * kTile, j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
+        // this wave's columns
+        const int column = 32 * wave + l;
+        const bool real = column < columns;
+        const int x = r0 + (real ? column : 0), j = over_g(x), r = x - j * a.g, pos = len - rows + j0 + j;
+        const int vhi = real ? (a.all ? len : min(pos + 1, len)) : 0, vlo = real && a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+        int some_lo = 0x7fffffff, some_hi = 0, all_lo = 0, all_hi = 0x7fffffff;
+        if (32 * wave < columns) {
+            const int pos0 = len - rows + j0 + over_g(r0 + 32 * wave), pos1 = len - rows + j0 + over_g(r0 + min(32 * wave + 31, columns - 1));
+            some_lo = a.window > 0 ? max(pos0 - a.window + 1, 0) : 0;
+            all_lo = a.window > 0 ? max(pos1 - a.window + 1, 0) : 0;
+            some_hi = a.all ? len : min(pos1 + 1, len);
+            all_hi = a.all ? len : min(pos0 + 1, len);
+        }
+        // a thread's words of a stage (its block of the two; past the end the last one's again)
+        const int* table = a.v.table + (size_t)max(slot, 0) * a.v.max_pages;
+        const int last_block = max((len + kKvBlock - 1) / kKvBlock - 1, 0);
+        int held = -64, pages = 0;
+        const auto fetch = [&](int stage, tile_words<D>& w) {
+            const int k = min(2 * stage + bk, last_block), f = k >> a.v.page_shift;
+            if (f >= held + 64) {
+                held = f;
+                pages = (int)min((unsigned)table[min(f + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
+            }
+            const unsigned char* block = kv_block<D>(a.v, __builtin_amdgcn_readlane(pages, f - held), head, k);
+            if constexpr (N == 2) {
+                const uint2 kw = *(const uint2*)(block + in_block), vw = *(const uint2*)(block + essa_k::kv_values_at(D) + in_block);
+                w.k[0] = kw.x;
+                w.k[1] = kw.y;
+                w.v[0] = vw.x;
+                w.v[1] = vw.y;
+            } else {
+                w.k[0] = *(const uint32_t*)(block + in_block);
+                w.v[0] = *(const uint32_t*)(block + essa_k::kv_values_at(D) + in_block);
+            }
+            w.k_scale = *(const uint16_t*)(block + k_scale_at) | (uint32_t)*(const uint16_t*)(block + k_scale_at + 16) << 16;
+            w.v_s = *(const u32x4*)(block + v_scale_at);
+            w.v_m = *(const u32x4*)(block + v_scale_at + 16);
+        };
+        const code_masks masks;
+        const auto unpack = [&](uint32_t w, f16x2 (&c)[4]) {   // q of eight elements
+            const f16x2 near = {(_Float16)-1032.f, (_Float16)-1032.f}, far = {(_Float16)-72.f, (_Float16)-72.f}, part = {(_Float16)0.0625f, (_Float16)0.0625f};
+            const uint32_t u = w >> 8;
+            c[0] = as_f16((w & masks.near) | masks.magic) + near;
+            c[1] = as_f16((w & masks.far) | masks.magic) * part + far;
+            c[2] = as_f16((u & masks.near) | masks.magic) + near;
+            c[3] = as_f16((u & masks.far) | masks.magic) * part + far;
+        };
+        const auto store = [&](int stage, tile_words<D>& w) {
+            tile_lds<D>& to = buffer[stage & 1];
+            const f16x2 ks = as_f16(w.k_scale & 0xffffu | w.k_scale << 16), km = as_f16(w.k_scale >> 16 | w.k_scale & 0xffff0000u);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                f16x2 c[4];
+                unpack(w.k[i], c);
+                u32x4 y;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * ks + km);
+                *(u32x4*)(to.k + k_to + 64 * i) = y;           // a lane's next word is 32 channels on
+            }
+            const int t0 = kStage * stage + 32 * bk;
+            if (t0 + 32 > len) {                               // past the end: nothing, whatever the page holds
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = t0 + (i & 3) + 16 * (i >> 2) + 4 * v_h;
+                    const uint32_t m = t < len ? ~0u : i & 1 ? 0x0000ffffu : 0xffff0000u;
+                    w.v_s[i >> 1] &= m;
+                    w.v_m[i >> 1] &= m;
+                }
+            }
+            typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+            u16x2 big = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, w.v_s[i] & 0x7fff7fffu));
+            if (max(big[0], big[1]) >= 0x7c00) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((w.v_s[i >> 1] >> (16 * (i & 1)) & 0x7c00u) == 0x7c00u) {
+                        const int t = 32 * bk + (i & 3) + 16 * (i >> 2) + 4 * v_h;
+                        atomicOr(&nans[stage % 3][v_chan / kKvGroup], 1ull << t);
+                        const uint32_t m = i & 1 ? 0x0000ffffu : 0xffff0000u;
+                        w.v_s[i >> 1] &= m;
+                        w.v_m[i >> 1] &= m;
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                f16x2 c[4];
+                unpack(w.v[i], c);
+                uint32_t y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * as_f16(w.v_s[k]) + as_f16(w.v_m[k]));
+                *(uint2*)(to.v + v_to + 16 * VROW * i) = uint2{y[0], y[1]};    // tokens 4 h ..
+                *(uint2*)(to.v + v_to + 16 * VROW * i + 32) = uint2{y[2], y[3]};                   // tokens 16 + 4 h ..
+            }
+        };
+        tile_words<D> ahead;
+        if (first < stop) fetch(first, ahead);
+        // queries: channels 16 k + 8 hh .. + 7, times a power of two
+        f16x8 q[KK];
+        float kappa, sum;
+        {
+            uint32_t raw[KK][4];
+            const long long q_at = (long long)(row0 + j0 + j) * a.Q.stride + (long long)(head * a.g + r) * D + 8 * hh;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) load_raw(a.Q, q_at + 16 * k, raw[k]);
+            typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+            u16x2 big2 = {0, 0};
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) big2 = __builtin_elementwise_max(big2, __builtin_bit_cast(u16x2, raw[k][i] & 0x7fff7fffu));
+            int big = max((int)big2[0], (int)big2[1]);
+            big = max(big, __shfl_xor(big, 32));
+            const bool finite = big < 0x7f80;
+            const int up = finite ? min(7 - (max(big >> 7, 1) - 127), 120) : 0;
+            const uint32_t keep = real && finite ? ~0u : 0u;
+            const float f = __uint_as_float((uint32_t)(127 + up) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t y = raw[k][i] & keep;
+                    q[k][2 * i] = (_Float16)(__uint_as_float(y << 16) * f);
+                    q[k][2 * i + 1] = (_Float16)(__uint_as_float(y & 0xffff0000u) * f);
+                }
+            kappa = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up) << 23);
+            sum = real && !finite && vlo < vhi ? NAN : 0.f;
+        }
+        const float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
+        float top = -kFar, down = kTileLift;
+        f32x16 o[OT];
+#pragma unroll
+        for (int i = 0; i < OT; ++i)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[i][k] = 0.f;
+        if (threadIdx.x < 3 * NG) nans[threadIdx.x / NG][threadIdx.x % NG] = 0;
+        lds_barrier();                                         // the buffers are free
+        if (first < stop) {
+            store(first, ahead);
+            if (first + 1 < stop) fetch(first + 1, ahead);
+        }
+        lds_barrier();
+        for (int stage = first; stage < stop; ++stage) {
+            const int t0 = kStage * stage;
+            const tile_lds<D>& now = buffer[stage & 1];
+            if (threadIdx.x < NG) nans[(stage + 2) % 3][threadIdx.x] = 0;
+            if (t0 < some_hi && t0 + kStage > some_lo) {
+                f32x16 s[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[i][k] = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KK; ++k)
+                        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)(now.k + (32 * i + l) * KROW + 32 * k + 16 * hh), q[k], s[i], 0, 0, 0);
+                }
+                const bool whole = t0 >= all_lo && t0 + kStage <= all_hi;
+                if (!whole) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const int t = t0 + 32 * i + (k & 3) + 8 * (k >> 2) + 4 * hh;
+                            s[i][k] = t >= vlo && t < vhi ? s[i][k] : -INFINITY;
+                        }
+                }
+                float m = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+                for (int k = 1; k < 16; ++k) m = fmaxf(fmaxf(m, s[0][k]), s[1][k]);
+                if (__any(m > top + slack)) {
+                    m = fmaxf(m, __shfl_xor(m, 32));
+                    const float new_top = fmaxf(top, m);
+                    const float f = new_top == top ? 1.f : __builtin_amdgcn_exp2f(fmaxf(top - new_top, -kFar) * kappa);
+                    top = new_top;
+                    down = fmaf(-new_top, kappa, kTileLift);
+                    down = new_top > -kFar ? down : kTileLift;
+                    sum *= f;
+#pragma unroll
+                    for (int i = 0; i < OT; ++i) o[i] *= f;
+                }
+                f16x8 p[2][2];
+                const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        float x[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            x[u] = __builtin_amdgcn_exp2f(fmaf(s[i][k + u], kappa, down));
+                            // an unseen score is -inf: its weight is 0, but for kappa = 0, where the product is NaN
+                            if (!whole) x[u] = s[i][k + u] == -INFINITY ? 0.f : x[u];
+                        }
+                        const f16x2 p2 = {(_Float16)x[0], (_Float16)x[1]};
+                        sum = __builtin_amdgcn_fdot2(p2, one, sum, false);
+                        p[i][k >> 3][k & 7] = p2[0];
+                        p[i][k >> 3][(k & 7) + 1] = p2[1];
+                    }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                        for (int ot = 0; ot < OT; ++ot)
+                            o[ot] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)(now.v + (32 * ot + l) * VROW + 64 * i + 32 * ks + 16 * hh), p[i][ks], o[ot], 0, 0, 0);
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) {
+                    const unsigned long long bad = nans[stage % 3][gr];
+                    if (bad) {
+                        bool sees = false;
+                        for (int t = 0; t < kStage; ++t) sees |= (bad >> t & 1) && t0 + t >= vlo && t0 + t < vhi;
+                        if (sees)
+#pragma unroll
+                            for (int ot = 0; ot < 2; ++ot)
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) o[2 * gr + ot][k] = NAN;
+                    }
+                }
+            }
+            if (stage + 1 < stop) {
+                store(stage + 1, ahead);
+                if (stage + 2 < stop) fetch(stage + 2, ahead);
+            }
+            lds_barrier();
+        }
+        sum += __shfl_xor(sum, 32);
+        const auto finish = [&](int col, int c, const f32x4& y, float weight) {
+            const int x = r0 + col, j = over_g(x);
+            put_out(a.Y, (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + x - j * a.g) * D + c,
+                    weight == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * __builtin_amdgcn_rcpf(weight));
+        };
+        if (real) {
+            const float best = top > -kFar ? top * kappa : -kFar;
+#pragma unroll
+            for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const f32x4 y = {o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]};
+                    const int c = 32 * ot + 8 * k + 4 * hh;
+                    if (complete) finish(column, c, y, sum);
+                    else put_part<D, kTile>(a.parts, 2 * (long long)blockIdx.x + begins, column, c, y, sum, best);
+                }
+        }
+        if (complete) continue;
+        join_parts<D, kTile, kTileThreads>(a.parts, a.done, divide(unit_at + kTileCost, part), divide(unit_at + size - 1, part), columns, &last_one, finish);
+    }
+}
+
 }  // namespace
 
 namespace essa_k {
 
-constexpr int kStreams = kKvAttnWorkgroups;
+constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // a CU each
 
-size_t kv_attention_bytes(const kv_view&, int D, int, const kv_rows&, int) { return (size_t)2 * kStreams * kColumns * (D + 4) * sizeof(float); }
+static size_t tile_count(int g, const kv_rows& rows) { return (size_t)((long long)rows.R * g / kTile) + rows.n + 1; }
+static size_t tile_words_of(int g, const kv_rows& rows) { return (3 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
+static bool may_have_prompts(int x_dtype, int g, const kv_rows& rows) {
+    return x_dtype == ESSA_BF16 && rows.row_start && rows.R > 1 && (long long)rows.R * g > kColumns;
+}
+
+size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& rows, int x_dtype) {
+    const int g = q_heads / v.heads;
+    const size_t streams = (size_t)2 * kStreams * kColumns * (D + 4) * sizeof(float);
+    if (!may_have_prompts(x_dtype, g, rows)) return streams;
+    return std::max(streams, (size_t)2 * kPrompts * kTile * (D + 4) * sizeof(float)) + tile_words_of(g, rows) * sizeof(int);
+}
 
 template <int D>
-static hipError_t run(hipStream_t st, attn_args a, void* ws, bool f32) {
-    a.parts = (float*)ws;
+static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     a.least = 16;
-    // the row of units at its longest: every entry as long as the table allows
-    const double longest = ((double)a.rows.R * a.g / kColumns + a.rows.n) * a.v.heads;
-    while (longest * (((long long)a.v.max_pages << a.v.page_shift >> a.grain) + kUnitCost + 1) > 1e9 && a.grain < 26) ++a.grain;
+    a.tile_least = 8;
+    // the rows of units at their longest: every entry as long as the table allows
+    const double units = ((double)a.rows.R * a.g / kColumns + a.rows.n) * a.v.heads, tiles = ((double)a.rows.R * a.g / kTile + a.rows.n) * a.v.heads;
+    const double blocks = (double)((long long)a.v.max_pages << a.v.page_shift);
+    while (units * (blocks / (1 << a.grain) + kUnitCost + 1) > 1e9 && a.grain < 26) ++a.grain;
+    while (tiles * (blocks / 2 / (1 << a.tile_grain) + kTileCost + 1) > 1e9 && a.tile_grain < 25) ++a.tile_grain;
+    const bool prompts = may_have_prompts(x_dtype, a.g, a.rows);
+    if (prompts) {
+        const size_t n = tile_count(a.g, a.rows);
+        a.tile = (int2*)ws;
+        a.tile_at = (int*)(a.tile + n);
+        a.tiles = a.tile_at + n + 1;
+        ws = (int*)ws + tile_words_of(a.g, a.rows);
+    }
+    a.parts = (float*)ws;
     const size_t lds = list_bytes(a.rows.n);
-    if (f32) kv_attn_stream_kernel<D, true><<<kStreams, 256, lds, st>>>(a);
+    if (x_dtype == ESSA_F32) kv_attn_stream_kernel<D, true><<<kStreams, 256, lds, st>>>(a);
     else kv_attn_stream_kernel<D, false><<<kStreams, 256, lds, st>>>(a);
+    if (prompts) kv_attn_prompt_kernel<D><<<kPrompts, kTileThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -728,7 +1175,7 @@ hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor
     a.window = window;
     a.all = all;
     a.done = done;
-    return D == 64 ? run<64>(st, a, ws, Q.dtype == ESSA_F32) : run<128>(st, a, ws, Q.dtype == ESSA_F32);
+    return D == 64 ? run<64>(st, a, ws, Q.dtype) : run<128>(st, a, ws, Q.dtype);
 }
 
 }  // namespace essa_k
