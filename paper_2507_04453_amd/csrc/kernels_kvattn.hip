@@ -54,11 +54,12 @@ __device__ __forceinline__ int wave_scan(int x, Op op) {
 // another -- of one entry and key head, over the blocks that the entry's rows see.  The units of all entries stand in one
 // row, each as long as its blocks and kUnitCost more (what it costs to begin and end one), and every workgroup takes the
 // same length of it: sequences of very different lengths keep the whole chip busy to the end.  A unit that lies in several
-// workgroups' parts is joined by the last of them to finish, in the order of the parts.  Where there are fewer units than
-// workgroups and all are short, a workgroup takes a whole one and nothing is joined.
+// workgroups' parts is joined by the last of them to finish, in the order of the parts.  A boundary that would leave less
+// than kSnap of a unit on one side moves to the unit's end: short units are never cut.  Where there are fewer units than
+// workgroups and all are short, a workgroup takes a whole one.
 // Lengths are counted in grains of 2^grain blocks: one block, unless the row could grow past an int.
 // ---------------------------------------------------------------------------------------------
-constexpr int kColumns = 64, kUnitCost = 4, kShort = 40;
+constexpr int kColumns = 64, kUnitCost = 4, kSnap = 12, kShort = 40;
 
 struct attn_args {
     kv_view v;
@@ -75,10 +76,10 @@ struct attn_args {
     // prompts: tiles of kTile columns of an entry, one after another, and how far the units before a tile reach
     int* tiles;                // [1] how many; null: this call has none
     int* tile_at;              // [tiles + 1]
-    int2* tile;                // [tiles] entry, which of its tiles
+    int4* tile;                // [2 tiles] slot, len, row0, rows of the entry; which of its tiles, first stage, stages, length of a unit
     int tile_grain, tile_least;
 };
-constexpr int kTile = 256, kStage = 64, kTileCost = 3;
+constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
 // An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16): there a
 // block is unpacked once for 256 columns instead of once for 16.  At 65 columns and 4000 tokens the two kernels are even.
 template <bool F32>
@@ -232,16 +233,26 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
             }
             const int4 e = l.entry[b];
             const tile_span t = tile_of(a, e.y, e.w, i - first[b]);
-            size = (((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost) * a.v.heads;
+            size = ((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost;
+            a.tile[2 * i] = e;
+            a.tile[2 * i + 1] = int4{i - first[b], t.lo, t.n, size};
         }
-        const int before = done + block_scan(size, total);
-        if (i < tiles) {
-            a.tile[i] = int2{b, i - first[b]};
-            a.tile_at[i] = before;
-        }
+        const int before = done + block_scan(size * a.v.heads, total);
+        if (i < tiles) a.tile_at[i] = before;
         done += total;
     }
     if (threadIdx.x == 0) a.tile_at[tiles] = done;
+}
+
+// Where a boundary at `at` goes, `off` into a unit of length `size`; and which parts the unit at `unit_at` then lies in.
+template <int SNAP>
+__device__ __forceinline__ int snapped(int at, int off, int size) { return off < SNAP ? at - off : size - off < SNAP ? at - off + size : at; }
+struct part_range {
+    int first, last;
+};
+template <int SNAP>
+__device__ __forceinline__ part_range parts_of(int unit_at, int size, int part) {
+    return {divide(unit_at + SNAP - 1, part), divide(unit_at + size - SNAP, part)};
 }
 
 // Parts of units that other workgroups read: written through to where every XCD sees them, and read from there, eight bytes
@@ -673,16 +684,38 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 4;
     const int total = uniform(list.at[a.rows.n]), part = list.even ? list.even : max(divide(total, (int)gridDim.x) + 1, a.least);
     const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
-    const int begin = part < 0x7fffffff / (int)gridDim.x ? blockIdx.x * part : (int)min((long long)blockIdx.x * part, 0x7fffffffll);
-    const int end = total - begin < part ? total : begin + part;
-    for (int at = begin; at < end;) {
+    struct place {
+        int4 entry;
+        entry_span sp;
+        int unit, unit_at, size, grains;
+    };
+    const auto place_of = [&](int at) {
         const int b = uniform(entry_at(list, a.rows.n, at));
         const int4 e = list.entry[b];
-        const int slot = uniform(e.x), len = uniform(e.y), row0 = uniform(e.z), rows = uniform(e.w);
-        const entry_span sp = span_of(a, len, rows);
-        const int in = uniform(at - list.at[b]), grains = ((sp.n - 1) >> a.grain) + 1, size = list.even ? list.even : grains + kUnitCost;
-        const int unit = divide(in, size), unit_at = at - (in - unit * size);
-        // the unit's blocks lie behind its cost: what a part has of the cost alone is no work
+        place p;
+        p.entry = int4{uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w)};
+        p.sp = span_of(a, p.entry.y, p.entry.w);
+        p.grains = ((p.sp.n - 1) >> a.grain) + 1;
+        p.size = list.even ? list.even : p.grains + kUnitCost;
+        const int in = uniform(at - list.at[b]);
+        p.unit = divide(in, p.size);
+        p.unit_at = at - (in - p.unit * p.size);
+        return p;
+    };
+    const auto boundary = [&](int w) {
+        if (w > divide(total, part)) return total;
+        const int at = w * part;
+        if (at >= total || list.even || w == 0) return min(at, total);
+        const place p = place_of(at);
+        return snapped<kSnap>(at, at - p.unit_at, p.size);
+    };
+    const int end = boundary(blockIdx.x + 1);
+    for (int at = boundary(blockIdx.x); at < end;) {
+        const place here = place_of(at);
+        const int slot = here.entry.x, len = here.entry.y, row0 = here.entry.z, rows = here.entry.w;
+        const entry_span sp = here.sp;
+        const int unit = here.unit, unit_at = here.unit_at, size = here.size, grains = here.grains;
+        // the unit's blocks lie behind its cost
         const int from = max(at - unit_at - kUnitCost, 0), to = min(min(size, end - unit_at) - kUnitCost, grains);
         at = unit_at + size;
         if (to <= from) continue;
@@ -781,7 +814,8 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
             else put_part<D, kColumns>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
         }
         if (complete) continue;
-        join_parts<D, kColumns, 256>(a.parts, a.done, divide(unit_at + kUnitCost, part), divide(unit_at + size - 1, part), columns, &last_one, finish);
+        const part_range parts = parts_of<kSnap>(unit_at, size, part);
+        join_parts<D, kColumns, 256>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
     // rows that see nothing: no unit holds them
     for (int b = blockIdx.x; b < a.rows.n; b += gridDim.x)
@@ -835,8 +869,26 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), l = lane & 31, hh = lane >> 5;
     const int total = uniform(a.tile_at[tiles]), part = max(divide(total, (int)gridDim.x) + 1, a.tile_least);
     const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
-    const int begin = part < 0x7fffffff / (int)gridDim.x ? blockIdx.x * part : (int)min((long long)blockIdx.x * part, 0x7fffffffll);
-    const int end = total - begin < part ? total : begin + part;
+    const auto tile_at = [&](int at) {                         // the tile that position `at` of the row lies in
+        int ti = 0;
+        for (int hi = tiles; hi - ti > 1;) {
+            const int step = (hi - ti + 63) / 64, t = ti + lane * step;
+            const unsigned long long below = __ballot(t < hi && a.tile_at[min(t, tiles)] <= at) | 1;
+            ti += (63 - __builtin_clzll(below)) * step;
+            hi = min(hi, ti + step);
+        }
+        return uniform(ti);
+    };
+    const auto boundary = [&](int w) {
+        if (w > divide(total, part)) return total;
+        const int at = w * part;
+        if (at >= total || w == 0) return min(at, total);
+        const int ti = tile_at(at), size = uniform(a.tile[2 * ti + 1].w), in = at - uniform(a.tile_at[ti]);
+        return snapped<kTileSnap>(at, in - divide(in, size) * size, size);
+    };
+    const int end = boundary(blockIdx.x + 1);
+    int at = boundary(blockIdx.x);
+    if (at >= end) return;
     // where this thread's words lie in a block, and where they go in LDS
     const int piece = threadIdx.x & 255, bk = wave >> 2, my_lane = N == 2 ? (piece & 127) >> 1 : piece >> 2;
     const int k_word = N == 2 ? 4 * (piece >> 7) + 2 * (piece & 1) : piece & 3;                    // w of the layout: token tile and step of 32 channels
@@ -848,28 +900,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
     const int k_to = (32 * bk + k_tok) * KROW + 2 * k_chan;
     const int v_to = v_chan * VROW + 64 * bk + 16 * (v_h & 1) + 8 * (v_h >> 1);
 
-    for (int at = begin; at < end;) {
-        int ti = 0;
-        for (int hi = tiles; hi - ti > 1;) {
-            const int step = (hi - ti + 63) / 64, t = ti + lane * step;
-            const unsigned long long below = __ballot(t < hi && a.tile_at[min(t, tiles)] <= at) | 1;
-            ti += (63 - __builtin_clzll(below)) * step;
-            hi = min(hi, ti + step);
-        }
-        ti = uniform(ti);
-        const int b = uniform(a.tile[ti].x), which = uniform(a.tile[ti].y);
-        kv_entry e = kv_entry_of(a.v, a.rows, b);
-        const int slot = uniform(e.slot), len = uniform(e.len), row0 = uniform(e.row0), rows = uniform(e.rows);
-        const tile_span sp = tile_of(a, len, rows, which);
-        const int in = at - uniform(a.tile_at[ti]), grains = (sp.n + (1 << a.tile_grain) - 1) >> a.tile_grain, size = grains + kTileCost;
-        const int head = divide(in, size), unit_at = at - (in - head * size);
+    int ti = tile_at(at), head, unit_at;
+    {
+        const int size = uniform(a.tile[2 * ti + 1].w), in = at - uniform(a.tile_at[ti]);
+        head = divide(in, size);
+        unit_at = at - (in - head * size);
+    }
+    // units in order: a tile's key heads, then the next tile's
+    for (; at < end; unit_at = at, ti += head + 1 == a.v.heads, head = head + 1 == a.v.heads ? 0 : head + 1) {
+        const int4 e = a.tile[2 * ti], t = a.tile[2 * ti + 1];
+        const int slot = uniform(e.x), len = uniform(e.y), row0 = uniform(e.z), rows = uniform(e.w);
+        const int which = uniform(t.x), tile_lo = uniform(t.y), tile_n = uniform(t.z), size = uniform(t.w), grains = size - kTileCost;
         const int from = max(at - unit_at - kTileCost, 0), to = min(min(size, end - unit_at) - kTileCost, grains);
         at = unit_at + size;
         const bool begins = from == 0, complete = begins && to == grains;
-        if (grains > 0 && to <= from) continue;
-        if (grains == 0 && unit_at + kTileCost > end) continue;                // no row sees anything: whoever has all of its cost writes the zeros
-        const int first = sp.lo + (from << a.tile_grain), stop = sp.lo + min(to << a.tile_grain, sp.n);
-        const int columns = sp.columns, c0 = which * kTile, j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
+        const int first = tile_lo + (from << a.tile_grain), stop = tile_lo + min(to << a.tile_grain, tile_n);
+        const int c0 = which * kTile, columns = (int)min((long long)rows * a.g - c0, (long long)kTile), j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
         // this wave's columns
         const int column = 32 * wave + l;
         const bool real = column < columns;
@@ -1114,7 +1160,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 }
         }
         if (complete) continue;
-        join_parts<D, kTile, kTileThreads>(a.parts, a.done, divide(unit_at + kTileCost, part), divide(unit_at + size - 1, part), columns, &last_one, finish);
+        const part_range parts = parts_of<kTileSnap>(unit_at, size, part);
+        join_parts<D, kTile, kTileThreads>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
 }
 
@@ -1125,7 +1172,7 @@ namespace essa_k {
 constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // a CU each
 
 static size_t tile_count(int g, const kv_rows& rows) { return (size_t)((long long)rows.R * g / kTile) + rows.n + 1; }
-static size_t tile_words_of(int g, const kv_rows& rows) { return (3 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
+static size_t tile_words_of(int g, const kv_rows& rows) { return (9 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
 static bool may_have_prompts(int x_dtype, int g, const kv_rows& rows) {
     return x_dtype == ESSA_BF16 && rows.row_start && rows.R > 1 && (long long)rows.R * g > kColumns;
 }
@@ -1149,8 +1196,8 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     const bool prompts = may_have_prompts(x_dtype, a.g, a.rows);
     if (prompts) {
         const size_t n = tile_count(a.g, a.rows);
-        a.tile = (int2*)ws;
-        a.tile_at = (int*)(a.tile + n);
+        a.tile = (int4*)ws;
+        a.tile_at = (int*)(a.tile + 2 * n);
         a.tiles = a.tile_at + n + 1;
         ws = (int*)ws + tile_words_of(a.g, a.rows);
     }
