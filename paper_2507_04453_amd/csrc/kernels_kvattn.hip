@@ -832,15 +832,36 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
 //
 // Scores^T = K Q^T and O^T = V^T P^T on the 32 x 32 x 16 MFMA.  Keys and values stand in LDS as fp16 numbers m + s q: rounded
 // once more (2^-11 of themselves) than in the stream kernel, because scales on the scores would be four multiply-adds for
-// each of them and the vector ALU is what this kernel is short of: 16 scores of a lane cost some 110 issue slots against 16
-// MFMAs.  Rows of LDS are 16 bytes longer than their values: every 16 lanes that read together meet 64 different banks.
-// The tokens of a value's row stand in the order in which the first product leaves the scores.  While a stage is worked on
-// the next one is unpacked into the other buffer and the one after it is on its way from memory; one barrier a stage.
+// each of them and the vector ALU is what this kernel is short of.  Rows of LDS are 16 bytes longer than their values: every
+// 16 lanes that read together meet 64 different banks.  The tokens of a value's row stand in the order in which the first
+// product leaves the scores.
+// The two waves of a SIMD take turns, a barrier between them: while one has the matrix cores (the values of its last stage,
+// the scores of its next) the other has the vector ALU (the weights of its stage, its share of unpacking a stage to come).
+// Left to themselves both did the same at the same time, and the time was the sum of the two.
 // A NaN among the values must not reach columns that do not see it (0 times NaN): it is taken out and noted, and the
-// columns that see it get theirs at the end of the stage.
+// columns that see it are made NaN.
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 constexpr int kTileThreads = 512;
+
+// N products with operands from LDS, some reads on their way in front of each (left alone, the compiler reads one operand
+// and waits for it): product(i, operand) for operand = *read(i).
+constexpr int kReadsAhead = 4;
+// between(i): something for the vector ALU after product i.
+template <int N, class Read, class Product, class Between>
+__device__ __forceinline__ void with_reads_ahead(Read read, Product product, Between between) {
+    f16x8 x[kReadsAhead];
+#pragma unroll
+    for (int i = 0; i < kReadsAhead; ++i) x[i] = *read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        product(i, x[i % kReadsAhead]);
+        if (i + kReadsAhead < N) x[i % kReadsAhead] = *read(i + kReadsAhead);
+        between(i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 template <int D>
 struct tile_lds {
@@ -861,8 +882,8 @@ struct tile_words {
 template <int D>
 __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_args a) {
     constexpr int N = D / 64, KK = D / 16, OT = D / 32, QUADS = D / 4, NG = D / kKvGroup, KROW = tile_lds<D>::KROW, VROW = tile_lds<D>::VROW;
-    __shared__ tile_lds<D> buffer[2];
-    __shared__ unsigned long long nans[3][NG];                 // tokens of a stage whose values are NaN, stage i's in i % 3
+    __shared__ tile_lds<D> buffer[3];
+    __shared__ unsigned nans[4][2 * NG + 1];                   // stage i's in i % 4: tokens whose values are NaN, by group; whether there are any
     __shared__ int last_one;
     const int tiles = uniform(*a.tiles);
     if (tiles == 0) return;
@@ -939,20 +960,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 held = f;
                 pages = (int)min((unsigned)table[min(f + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
             }
-            const unsigned char* block = kv_block<D>(a.v, __builtin_amdgcn_readlane(pages, f - held), head, k);
+            // (a scalar base and 32-bit offsets: registers are short here)
+            const rsrc_t block = make_rsrc(kv_block<D>(a.v, __builtin_amdgcn_readlane(pages, f - held), head, k));
             if constexpr (N == 2) {
-                const uint2 kw = *(const uint2*)(block + in_block), vw = *(const uint2*)(block + essa_k::kv_values_at(D) + in_block);
+                const uint2 kw = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(block, in_block, 0, 0));
+                const uint2 vw = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(block, in_block, essa_k::kv_values_at(D), 0));
                 w.k[0] = kw.x;
                 w.k[1] = kw.y;
                 w.v[0] = vw.x;
                 w.v[1] = vw.y;
             } else {
-                w.k[0] = *(const uint32_t*)(block + in_block);
-                w.v[0] = *(const uint32_t*)(block + essa_k::kv_values_at(D) + in_block);
+                w.k[0] = __builtin_amdgcn_raw_buffer_load_b32(block, in_block, 0, 0);
+                w.v[0] = __builtin_amdgcn_raw_buffer_load_b32(block, in_block, essa_k::kv_values_at(D), 0);
             }
-            w.k_scale = *(const uint16_t*)(block + k_scale_at) | (uint32_t)*(const uint16_t*)(block + k_scale_at + 16) << 16;
-            w.v_s = *(const u32x4*)(block + v_scale_at);
-            w.v_m = *(const u32x4*)(block + v_scale_at + 16);
+            w.k_scale = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 0, 0) | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 16, 0) << 16;
+            w.v_s = load16(block, v_scale_at, 0);
+            w.v_m = load16(block, v_scale_at, 16);
         };
         const code_masks masks;
         const auto unpack = [&](uint32_t w, f16x2 (&c)[4]) {   // q of eight elements
@@ -963,24 +986,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             c[2] = as_f16((u & masks.near) | masks.magic) + near;
             c[3] = as_f16((u & masks.far) | masks.magic) * part + far;
         };
-        const auto store = [&](int stage, tile_words<D>& w) {
-            tile_lds<D>& to = buffer[stage & 1];
-            const f16x2 ks = as_f16(w.k_scale & 0xffffu | w.k_scale << 16), km = as_f16(w.k_scale >> 16 | w.k_scale & 0xffff0000u);
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                f16x2 c[4];
-                unpack(w.k[i], c);
-                u32x4 y;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * ks + km);
-                *(u32x4*)(to.k + k_to + 64 * i) = y;           // a lane's next word is 32 channels on
-            }
+        // what must not get into LDS: values behind the last token, whatever the page holds, and NaN
+        const auto clean = [&](int stage, tile_words<D>& w) {
             const int t0 = kStage * stage + 32 * bk;
-            if (t0 + 32 > len) {                               // past the end: nothing, whatever the page holds
+            if (t0 + 32 > len) {
+                int left = len - t0 - 4 * v_h;
+                asm volatile("" : "+v"(left));                 // rare paths keep nothing in registers for their sake
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int t = t0 + (i & 3) + 16 * (i >> 2) + 4 * v_h;
-                    const uint32_t m = t < len ? ~0u : i & 1 ? 0x0000ffffu : 0xffff0000u;
+                    const uint32_t half = i & 1 ? 0xffff0000u : 0xffffu;
+                    const uint32_t m = (i & 3) + 16 * (i >> 2) < left ? ~0u : ~half;
                     w.v_s[i >> 1] &= m;
                     w.v_m[i >> 1] &= m;
                 }
@@ -990,25 +1005,52 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
 #pragma unroll
             for (int i = 0; i < 4; ++i) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2, w.v_s[i] & 0x7fff7fffu));
             if (max(big[0], big[1]) >= 0x7c00) {
+                int from = 32 * bk + 4 * v_h;
+                asm volatile("" : "+v"(from));
+                nans[stage & 3][2 * NG] = 1;
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    const int sh = 16 * (i & 1);
+                    uint32_t word = w.v_s[0];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if ((w.v_s[i >> 1] >> (16 * (i & 1)) & 0x7c00u) == 0x7c00u) {
-                        const int t = 32 * bk + (i & 3) + 16 * (i >> 2) + 4 * v_h;
-                        atomicOr(&nans[stage % 3][v_chan / kKvGroup], 1ull << t);
-                        const uint32_t m = i & 1 ? 0x0000ffffu : 0xffff0000u;
-                        w.v_s[i >> 1] &= m;
-                        w.v_m[i >> 1] &= m;
+                    for (int k = 1; k < 4; ++k) word = k == i >> 1 ? w.v_s[k] : word;
+                    if ((word >> sh & 0x7c00u) == 0x7c00u) {
+                        const int t = from + (i & 3) + 16 * (i >> 2);
+                        atomicOr(&nans[stage & 3][2 * (v_chan / kKvGroup) + (t >> 5)], 1u << (t & 31));
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t m = k == i >> 1 ? ~(0xffffu << sh) : ~0u;
+                            w.v_s[k] &= m;
+                            w.v_m[k] &= m;
+                        }
                     }
+                }
             }
+        };
+        const auto store_keys = [&](int stage, const tile_words<D>& w, int i) {
+            const f16x2 ks = as_f16(w.k_scale & 0xffffu | w.k_scale << 16), km = as_f16(w.k_scale >> 16 | w.k_scale & 0xffff0000u);
+            f16x2 c[4];
+            unpack(w.k[i], c);
+            u32x4 y;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * ks + km);
+            *(u32x4*)(buffer[stage % 3].k + k_to + 64 * i) = y;                // a lane's next word is 32 channels on
+        };
+        const auto store_values = [&](int stage, const tile_words<D>& w, int i) {
+            f16x2 c[4];
+            unpack(w.v[i], c);
+            uint32_t y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * as_f16(w.v_s[k]) + as_f16(w.v_m[k]));
+            unsigned char* to = buffer[stage % 3].v + v_to + 16 * VROW * i;
+            *(uint2*)to = uint2{y[0], y[1]};                   // tokens 4 h ..
+            *(uint2*)(to + 32) = uint2{y[2], y[3]};            // tokens 16 + 4 h ..
+        };
+        const auto store = [&](int stage, const tile_words<D>& w) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                f16x2 c[4];
-                unpack(w.v[i], c);
-                uint32_t y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) y[k] = __builtin_bit_cast(uint32_t, c[k] * as_f16(w.v_s[k]) + as_f16(w.v_m[k]));
-                *(uint2*)(to.v + v_to + 16 * VROW * i) = uint2{y[0], y[1]};    // tokens 4 h ..
-                *(uint2*)(to.v + v_to + 16 * VROW * i + 32) = uint2{y[2], y[3]};                   // tokens 16 + 4 h ..
+                store_keys(stage, w, i);
+                store_values(stage, w, i);
             }
         };
         tile_words<D> ahead;
@@ -1031,7 +1073,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             big = max(big, __shfl_xor(big, 32));
             const bool finite = big < 0x7f80;
             const int up = finite ? min(7 - (max(big >> 7, 1) - 127), 120) : 0;
-            const uint32_t keep = real && finite ? ~0u : 0u;
+            kappa = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up) << 23);
+            // scores that do not count (scale = 0) are those of a zero query: exponents are formed with kappa > 0
+            const uint32_t keep = real && finite && kappa > 0.f ? ~0u : 0u;
+            kappa = kappa > 0.f ? kappa : 1.f;
             const float f = __uint_as_float((uint32_t)(127 + up) << 23 | (a.scale < 0.f ? 0x80000000u : 0u));
 #pragma unroll
             for (int k = 0; k < KK; ++k)
@@ -1041,7 +1086,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                     q[k][2 * i] = (_Float16)(__uint_as_float(y << 16) * f);
                     q[k][2 * i + 1] = (_Float16)(__uint_as_float(y & 0xffff0000u) * f);
                 }
-            kappa = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up) << 23);
             sum = real && !finite && vlo < vhi ? NAN : 0.f;
         }
         const float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
@@ -1051,96 +1095,117 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
         for (int i = 0; i < OT; ++i)
 #pragma unroll
             for (int k = 0; k < 16; ++k) o[i][k] = 0.f;
-        if (threadIdx.x < 3 * NG) nans[threadIdx.x / NG][threadIdx.x % NG] = 0;
+        if (threadIdx.x < 4 * (2 * NG + 1)) nans[threadIdx.x / (2 * NG + 1)][threadIdx.x % (2 * NG + 1)] = 0;
         lds_barrier();                                         // the buffers are free
         if (first < stop) {
+            clean(first, ahead);
             store(first, ahead);
-            if (first + 1 < stop) fetch(first + 1, ahead);
+            if (first + 1 < stop) {
+                fetch(first + 1, ahead);
+                clean(first + 1, ahead);
+                store(first + 1, ahead);
+            }
         }
         lds_barrier();
+        // Turns end at barriers.  Waves 0 .. 3 have the matrix cores at even turns, waves 4 .. 7 at odd ones.  Stage i (from 0)
+        // of a wave of half h: scores at turn 2 i + h, weights at 2 i + 1 + h, values at 2 i + 2 + h; it is unpacked at turns
+        // 2 i - 2 and 2 i - 1, between the products, so three buffers do.  A wave goes through all stages of the workgroup:
+        // where its columns see nothing the weights are 0.
+        const int half = wave >> 2;
+        f32x16 s[2];
+        f16x8 p[2][2];
+        const auto scores = [&](int stage, auto between) {
+            const unsigned char* from = buffer[stage % 3].k + l * KROW + 16 * hh;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) s[i][k] = 0.f;
+            with_reads_ahead<2 * KK>([&](int i) { return (const f16x8*)(from + 32 * KROW * (i & 1) + 32 * (i >> 1)); },
+                                     [&](int i, const f16x8& x) { s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[i >> 1], s[i & 1], 0, 0, 0); }, between);
+        };
+        if (half) lds_barrier();
+        if (first < stop) scores(first, [](int) {});
         for (int stage = first; stage < stop; ++stage) {
-            const int t0 = kStage * stage;
-            const tile_lds<D>& now = buffer[stage & 1];
-            if (threadIdx.x < NG) nans[(stage + 2) % 3][threadIdx.x] = 0;
-            if (t0 < some_hi && t0 + kStage > some_lo) {
-                f32x16 s[2];
+                lds_barrier();
+                if (threadIdx.x < 2 * NG + 1) nans[(stage + 2) & 3][threadIdx.x] = 0;
+                if (stage + 2 < stop) fetch(stage + 2, ahead);
+                {
+                    const int t0 = kStage * stage;
+                    const unsigned any_nan = nans[stage & 3][2 * NG];
+                    const bool whole = t0 >= all_lo && t0 + kStage <= all_hi;
+                    if (!whole) {
+                        int lo = vlo - t0 - 4 * hh, hi = vhi - t0 - 4 * hh;
+                        asm volatile("" : "+v"(lo), "+v"(hi)); // or every token's bounds stand in registers all the time
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) s[i][k] = 0.f;
+                            for (int k = 0; k < 16; ++k) {
+                                const int t = 32 * i + (k & 3) + 8 * (k >> 2);
+                                s[i][k] = t >= lo && t < hi ? s[i][k] : -INFINITY;
+                            }
+                    }
+                    float m = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-                    for (int k = 0; k < KK; ++k)
-                        s[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)(now.k + (32 * i + l) * KROW + 32 * k + 16 * hh), q[k], s[i], 0, 0, 0);
-                }
-                const bool whole = t0 >= all_lo && t0 + kStage <= all_hi;
-                if (!whole) {
+                    for (int k = 1; k < 16; ++k) m = fmaxf(fmaxf(m, s[0][k]), s[1][k]);
+                    if (__any(m > top + slack)) {
+                        m = fmaxf(m, __shfl_xor(m, 32));
+                        const float new_top = fmaxf(top, m);
+                        const float f = new_top == top ? 1.f : __builtin_amdgcn_exp2f(fmaxf(top - new_top, -kFar) * kappa);
+                        top = new_top;
+                        down = fmaf(-new_top, kappa, kTileLift);
+                        down = new_top > -kFar ? down : kTileLift;
+                        sum *= f;
+#pragma unroll
+                        for (int i = 0; i < OT; ++i) o[i] *= f;
+                    }
+                    const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const int t = t0 + 32 * i + (k & 3) + 8 * (k >> 2) + 4 * hh;
-                            s[i][k] = t >= vlo && t < vhi ? s[i][k] : -INFINITY;
+                        for (int k = 0; k < 16; k += 2) {
+                            const float x = __builtin_amdgcn_exp2f(fmaf(s[i][k], kappa, down)), y = __builtin_amdgcn_exp2f(fmaf(s[i][k + 1], kappa, down));
+                            const f16x2 p2 = {(_Float16)x, (_Float16)y};
+                            sum = __builtin_amdgcn_fdot2(p2, one, sum, false);
+                            p[i][k >> 3][k & 7] = p2[0];
+                            p[i][k >> 3][(k & 7) + 1] = p2[1];
+                        }
+                    if (any_nan)
+#pragma unroll
+                        for (int gr = 0; gr < NG; ++gr) {
+                            bool sees = false;
+#pragma unroll 1
+                            for (int t = 0; t < kStage; ++t) sees |= (nans[stage & 3][2 * gr + (t >> 5)] >> (t & 31) & 1) && t0 + t >= vlo && t0 + t < vhi;
+                            if (sees)
+#pragma unroll
+                                for (int ot = 0; ot < 2; ++ot)
+#pragma unroll
+                                    for (int k = 0; k < 16; ++k) o[2 * gr + ot][k] = NAN;
                         }
                 }
-                float m = fmaxf(s[0][0], s[1][0]);
+            // in this turn: the compiler would move the exponentials behind the barrier, to where they are used
 #pragma unroll
-                for (int k = 1; k < 16; ++k) m = fmaxf(fmaxf(m, s[0][k]), s[1][k]);
-                if (__any(m > top + slack)) {
-                    m = fmaxf(m, __shfl_xor(m, 32));
-                    const float new_top = fmaxf(top, m);
-                    const float f = new_top == top ? 1.f : __builtin_amdgcn_exp2f(fmaxf(top - new_top, -kFar) * kappa);
-                    top = new_top;
-                    down = fmaf(-new_top, kappa, kTileLift);
-                    down = new_top > -kFar ? down : kTileLift;
-                    sum *= f;
-#pragma unroll
-                    for (int i = 0; i < OT; ++i) o[i] *= f;
-                }
-                f16x8 p[2][2];
-                const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        float x[2];
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            x[u] = __builtin_amdgcn_exp2f(fmaf(s[i][k + u], kappa, down));
-                            // an unseen score is -inf: its weight is 0, but for kappa = 0, where the product is NaN
-                            if (!whole) x[u] = s[i][k + u] == -INFINITY ? 0.f : x[u];
-                        }
-                        const f16x2 p2 = {(_Float16)x[0], (_Float16)x[1]};
-                        sum = __builtin_amdgcn_fdot2(p2, one, sum, false);
-                        p[i][k >> 3][k & 7] = p2[0];
-                        p[i][k >> 3][(k & 7) + 1] = p2[1];
-                    }
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-                        for (int ot = 0; ot < OT; ++ot)
-                            o[ot] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)(now.v + (32 * ot + l) * VROW + 64 * i + 32 * ks + 16 * hh), p[i][ks], o[ot], 0, 0, 0);
-#pragma unroll
-                for (int gr = 0; gr < NG; ++gr) {
-                    const unsigned long long bad = nans[stage % 3][gr];
-                    if (bad) {
-                        bool sees = false;
-                        for (int t = 0; t < kStage; ++t) sees |= (bad >> t & 1) && t0 + t >= vlo && t0 + t < vhi;
-                        if (sees)
-#pragma unroll
-                            for (int ot = 0; ot < 2; ++ot)
-#pragma unroll
-                                for (int k = 0; k < 16; ++k) o[2 * gr + ot][k] = NAN;
-                    }
-                }
+            for (int i = 0; i < 4; ++i) {
+                u32x4 w = __builtin_bit_cast(u32x4, p[i >> 1][i & 1]);
+                asm volatile("" : "+v"(w));
+                p[i >> 1][i & 1] = __builtin_bit_cast(f16x8, w);
             }
-            if (stage + 1 < stop) {
-                store(stage + 1, ahead);
-                if (stage + 2 < stop) fetch(stage + 2, ahead);
-            }
+            asm volatile("" : "+v"(sum));
+            if (stage + 2 < stop) clean(stage + 2, ahead);
             lds_barrier();
+            __builtin_amdgcn_s_setprio(1);
+            const unsigned char* from = buffer[stage % 3].v + l * VROW + 16 * hh;
+            with_reads_ahead<4 * OT>([&](int i) { return (const f16x8*)(from + 32 * VROW * (i % OT) + 32 * (i / OT)); },
+                                     [&](int i, const f16x8& x) { o[i % OT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, p[i / OT >> 1][i / OT & 1], o[i % OT], 0, 0, 0); },
+                                     [&](int i) {              // past the last stage: into a buffer that nobody reads
+                                         if (i % 8 == 4) store_keys(stage + 2, ahead, i / 8);
+                                     });
+            scores(stage + 1, [&](int i) {                     // past the last stage: of what lies there, not looked at
+                if (i % 8 == 4) store_values(stage + 2, ahead, i / 8);
+            });
+            __builtin_amdgcn_s_setprio(0);
         }
+        lds_barrier();
+        if (!half) lds_barrier();
         sum += __shfl_xor(sum, 32);
         const auto finish = [&](int col, int c, const f32x4& y, float weight) {
             const int x = r0 + col, j = over_g(x);
