@@ -875,7 +875,7 @@ template <int D>
 struct tile_words {
     static constexpr int N = D / 64;
     uint32_t k[N], v[N];
-    uint32_t k_scale;          // s in the low half, m in the high one
+    uint32_t k_s, k_m;         // 16 bits each; put together where they are used, or the loads would be waited for where they are issued
     u32x4 v_s, v_m;
 };
 
@@ -973,7 +973,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 w.k[0] = __builtin_amdgcn_raw_buffer_load_b32(block, in_block, 0, 0);
                 w.v[0] = __builtin_amdgcn_raw_buffer_load_b32(block, in_block, essa_k::kv_values_at(D), 0);
             }
-            w.k_scale = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 0, 0) | (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 16, 0) << 16;
+            w.k_s = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 0, 0);
+            w.k_m = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(block, k_scale_at, 16, 0);
             w.v_s = load16(block, v_scale_at, 0);
             w.v_m = load16(block, v_scale_at, 16);
         };
@@ -1028,7 +1029,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             }
         };
         const auto store_keys = [&](int stage, const tile_words<D>& w, int i) {
-            const f16x2 ks = as_f16(w.k_scale & 0xffffu | w.k_scale << 16), km = as_f16(w.k_scale >> 16 | w.k_scale & 0xffff0000u);
+            const f16x2 ks = as_f16(w.k_s | w.k_s << 16), km = as_f16(w.k_m | w.k_m << 16);
             f16x2 c[4];
             unpack(w.k[i], c);
             u32x4 y;
@@ -1053,16 +1054,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 store_values(stage, w, i);
             }
         };
-        tile_words<D> ahead;
-        if (first < stop) fetch(first, ahead);
+        // the queries and the first two stages' words, all on their way together
+        uint32_t raw[KK][4];
+        {
+            const long long q_at = (long long)(row0 + j0 + j) * a.Q.stride + (long long)(head * a.g + r) * D + 8 * hh;
+#pragma unroll
+            for (int k = 0; k < KK; ++k) load_raw(a.Q, q_at + 16 * k, raw[k]);
+        }
+        tile_words<D> ahead, second;
+        if (first < stop) {
+            fetch(first, ahead);
+            fetch(min(first + 1, stop - 1), second);
+        }
         // queries: channels 16 k + 8 hh .. + 7, times a power of two
         f16x8 q[KK];
         float kappa, sum;
         {
-            uint32_t raw[KK][4];
-            const long long q_at = (long long)(row0 + j0 + j) * a.Q.stride + (long long)(head * a.g + r) * D + 8 * hh;
-#pragma unroll
-            for (int k = 0; k < KK; ++k) load_raw(a.Q, q_at + 16 * k, raw[k]);
             typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
             u16x2 big2 = {0, 0};
 #pragma unroll
@@ -1101,9 +1108,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             clean(first, ahead);
             store(first, ahead);
             if (first + 1 < stop) {
-                fetch(first + 1, ahead);
-                clean(first + 1, ahead);
-                store(first + 1, ahead);
+                clean(first + 1, second);
+                store(first + 1, second);
             }
         }
         lds_barrier();
@@ -1190,8 +1196,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 p[i >> 1][i & 1] = __builtin_bit_cast(f16x8, w);
             }
             asm volatile("" : "+v"(sum));
-            if (stage + 2 < stop) clean(stage + 2, ahead);
             lds_barrier();
+            if (stage + 2 < stop) clean(stage + 2, ahead);
             __builtin_amdgcn_s_setprio(1);
             const unsigned char* from = buffer[stage % 3].v + l * VROW + 16 * hh;
             with_reads_ahead<4 * OT>([&](int i) { return (const f16x8*)(from + 32 * VROW * (i % OT) + 32 * (i / OT)); },
@@ -1212,17 +1218,47 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             put_out(a.Y, (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + x - j * a.g) * D + c,
                     weight == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * __builtin_amdgcn_rcpf(weight));
         };
-        if (real) {
+        if (complete) {
+            // a column's channels lie in 16 pieces of 8 bytes over its two lanes: through LDS (this wave's own 32 rows of it, the
+            // buffers are done with), so that rows go out whole
+            const float over = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);  // (where the sum is 0, so is the column)
+            constexpr int YROW = 2 * D + 16;
+            static_assert(kTileThreads / 2 * YROW <= sizeof buffer, "");
+            unsigned char* mine = (unsigned char*)buffer + 32 * wave * YROW;
+            if (a.Y.dtype == ESSA_BF16 && a.Y.aligned) {
+#pragma unroll
+                for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) w[i] = f32_to_bf16_bits(o[ot][4 * k + 2 * i] * over) | (uint32_t)f32_to_bf16_bits(o[ot][4 * k + 2 * i + 1] * over) << 16;
+                        *(uint2*)(mine + l * YROW + 2 * (32 * ot + 8 * k + 4 * hh)) = uint2{w[0], w[1]};
+                    }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {             // 64 lanes x 16 bytes: 512 / D rows at a time
+                    const int in = 64 * i + lane, row = in / (D / 8), c = 8 * (in % (D / 8)), col = 32 * wave + row;
+                    const int xx = r0 + col, jj = over_g(xx);
+                    if (col < columns)
+                        *(u32x4*)((uint16_t*)a.Y.p + (long long)(row0 + j0 + jj) * a.Y.stride + (long long)(head * a.g + xx - jj * a.g) * D + c) = *(const u32x4*)(mine + row * YROW + 2 * c);
+                }
+            } else if (real) {
+                const long long y_at = (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + r) * D + 4 * hh;
+#pragma unroll
+                for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        put_out(a.Y, y_at + 32 * ot + 8 * k, f32x4{o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]} * over);
+            }
+        } else if (real) {
             const float best = top > -kFar ? top * kappa : -kFar;
 #pragma unroll
             for (int ot = 0; ot < OT; ++ot)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const f32x4 y = {o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]};
-                    const int c = 32 * ot + 8 * k + 4 * hh;
-                    if (complete) finish(column, c, y, sum);
-                    else put_part<D, kTile>(a.parts, 2 * (long long)blockIdx.x + begins, column, c, y, sum, best);
-                }
+                for (int k = 0; k < 4; ++k)
+                    put_part<D, kTile>(a.parts, 2 * (long long)blockIdx.x + begins, column, 32 * ot + 8 * k + 4 * hh,
+                                       f32x4{o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]}, sum, best);
         }
         if (complete) continue;
         const part_range parts = parts_of<kTileSnap>(unit_at, size, part);
