@@ -59,7 +59,7 @@ __device__ __forceinline__ int wave_scan(int x, Op op) {
 // workgroups and all are short, a workgroup takes a whole one.
 // Lengths are counted in grains of 2^grain blocks: one block, unless the row could grow past an int.
 // ---------------------------------------------------------------------------------------------
-constexpr int kColumns = 64, kUnitCost = 4, kSnap = 12, kShort = 40;
+constexpr int kColumns = 64, kUnitCost = 6, kSnap = 9, kShort = 40;
 
 struct attn_args {
     kv_view v;
@@ -93,7 +93,7 @@ __device__ __forceinline__ entry_span span_of(const attn_args& a, int len, int r
     const int lo = a.window > 0 ? max(len - rows - a.window + 1, 0) : 0;
     s.lo = lo / kKvBlock;
     s.n = rows > 0 && len > 0 ? (len + kKvBlock - 1) / kKvBlock - s.lo : 0;
-    s.groups = (int)(((long long)rows * a.g + kColumns - 1) / kColumns);
+    s.groups = (int)(((unsigned)(rows * a.g) + kColumns - 1) / kColumns);      // R rows of q_heads are below 2^31
     return s;
 }
 
@@ -369,13 +369,13 @@ __device__ __forceinline__ void load_raw(const kv_tensor& Q, long long at, uint3
 //
 // Scores^T = K Q^T and O^T = V^T P^T, both with the tokens' side as the MFMA's first operand, so that the scores leave the
 // first product (column = lane % 16) in the order in which the second one takes its weights: no exchange between lanes.
-// Codes become operands by bit operations alone: 1024 + c in fp16 has c in its low bits, 1024 + 16 c the next four.  What is
-// too much is taken off in the sums: of keys by where the accumulators start, -sum (1032 q) (a far element's query is q / 16
-// and its 1152), of values by a product with a constant operand, -1032, in the same block, so that the accumulators never
-// hold more than one block's 1032 sum p s.  Scales and middles of a group go onto the scores and the weights:
+// Codes become operands by bit operations alone: 128 + c in bf16 and 1024 + c in fp16 have c in their low bits.  What is too
+// much is taken off in the sums: of keys by where the accumulators start, -136 sum q, of values by a product with a constant
+// operand, -1032, in the same block, so that the accumulators never hold more than one block's 1032 sum p s.  Scales and
+// middles of a group go onto the scores and the weights:
 //   score = sum_group s <q, c - 8> + m sum q,      O = sum_group (p s) (c - 8) + sum p m.
-// bf16 queries: q times a power of two in fp16 (exact but for what is 2^-22 of the row's largest), weights and weights times
-// scales in fp16, sums in fp32.  fp32 queries: the same on the fp32 MFMA, with c - 8 as operands.
+// bf16 queries: keys on the bf16 MFMA, every product exact; weights and weights times scales in fp16; sums in fp32.  fp32
+// queries: the same on the fp32 MFMA, with c - 8 as operands.
 // The running maximum moves only when a score passes it by 4 (in the exponent of 2), which after the first blocks is rare:
 // weights stay below 2^3 and times a scale (at most 4370) below the range of fp16.
 // ---------------------------------------------------------------------------------------------
@@ -417,21 +417,17 @@ __device__ __forceinline__ void fetch_block(uint32_t lds, const unsigned char* b
 
 __device__ __forceinline__ f16x2 as_f16(uint32_t w) { return __builtin_bit_cast(f16x2, w); }
 struct code_masks {            // in registers, or every use would be two instructions (a literal each)
-    uint32_t near = 0x000f000fu, far = 0x00f000f0u, magic = 0x64006400u;
+    uint32_t near = 0x000f000fu, far = 0x00f000f0u, magic = 0x64006400u, magic_bf16 = 0x43004300u;
     __device__ __forceinline__ code_masks() {
         asm volatile("" : "+v"(near));
         asm volatile("" : "+v"(far));
         asm volatile("" : "+s"(magic));
+        asm volatile("" : "+s"(magic_bf16));
     }
 };
-// elements 0, 1, 4, 5 as 1024 + c, the others as 1024 + 16 c (c = q + 8)
-__device__ __forceinline__ f16x8 codes_near_far(uint32_t w, const code_masks& m) {
-    const uint32_t u = w >> 8;
-    return __builtin_bit_cast(f16x8, u32x4{(w & m.near) | m.magic, (w & m.far) | m.magic, (u & m.near) | m.magic, (u & m.far) | m.magic});
-}
-// all as 1024 + c
-__device__ __forceinline__ f16x8 codes_near(uint32_t w, const code_masks& m) {
-    return __builtin_bit_cast(f16x8, u32x4{(w & m.near) | m.magic, (w >> 4 & m.near) | m.magic, (w >> 8 & m.near) | m.magic, (w >> 12 & m.near) | m.magic});
+// 1024 + c in fp16, 128 + c in bf16 (c = q + 8)
+__device__ __forceinline__ u32x4 codes_on(uint32_t w, uint32_t mask, uint32_t magic) {
+    return u32x4{(w & mask) | magic, (w >> 4 & mask) | magic, (w >> 8 & mask) | magic, (w >> 12 & mask) | magic};
 }
 __device__ __forceinline__ void codes_f32(uint32_t w, float (&c)[8]) {
 #pragma unroll
@@ -443,7 +439,7 @@ __device__ __forceinline__ float half_of(const u32x4& r, int e) { return (float)
 template <int D, bool F32>
 struct attn_state {
     static constexpr int NG = D / kKvGroup, KK = D / 32;
-    f16x8 q16[F32 ? 1 : KK];
+    bf16x8 q16[F32 ? 1 : KK];
     float q32[F32 ? KK : 1][8];
     float qsum[NG];            // sum of q over a group
     float less[NG];            // what the scores' accumulators start from
@@ -459,8 +455,11 @@ struct attn_state {
     // w: the lane's channels 32 k + 8 (lane / 16) .. + 7 as they are in memory; pos: position of the column's row; real: the column exists
     static constexpr int RAW = F32 ? 8 : 4;                    // words of 8 channels
     __device__ __forceinline__ void start(const attn_args& a, uint32_t (&w)[KK][RAW], int len, int pos, bool real) {
-        const uint32_t sign = a.scale < 0.f ? 0x80000000u : 0u;
+        // a negative scale is the queries' sign
+        const uint32_t sign = a.scale < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
         bool finite;
+#pragma unroll
+        for (int gr = 0; gr < NG; ++gr) qsum[gr] = 0.f;
         if constexpr (F32) {
             uint32_t big = 0;
 #pragma unroll
@@ -469,50 +468,40 @@ struct attn_state {
                 for (int i = 0; i < 8; ++i) big = max(big, w[k][i] & 0x7fffffffu);
             finite = quarters(__uint_as_float(big), [](float x, float y) { return __uint_as_float(max(__float_as_uint(x), __float_as_uint(y))); }) <= kFar;
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) qsum[gr] = less[gr] = 0.f;
-#pragma unroll
             for (int k = 0; k < KK; ++k)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     q32[k][i] = real && finite ? __uint_as_float(w[k][i] ^ sign) : 0.f;
                     qsum[32 * k / kKvGroup] += q32[k][i];
                 }
-            kappa = fabsf(a.scale);
         } else {
             typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+            typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
             u16x2 big2 = {0, 0};
 #pragma unroll
             for (int k = 0; k < KK; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) big2 = __builtin_elementwise_max(big2, __builtin_bit_cast(u16x2, w[k][i] & 0x7fff7fffu));
-            const int big = (int)quarters_max((float)max((int)big2[0], (int)big2[1]));             // below 2^15: exact as a float
-            finite = big < 0x7f80;
-            // 2^up brings the largest into 2^7 .. 2^8; cut at 2^120 for the smallest rows, which are exact all the same
-            const int up = finite ? min(7 - (max(big >> 7, 1) - 127), 120) : 0;
+            finite = quarters_max((float)max((int)big2[0], (int)big2[1])) < (float)0x7f80;         // bits below 2^15: exact as floats
             const uint32_t keep = real && finite ? ~0u : 0u;
-            const float near = __uint_as_float((uint32_t)(127 + up) << 23 | sign), far = 0.0625f * near;
-            const f16x2 one = {(_Float16)1.f, (_Float16)1.f}, sixteen = {(_Float16)16.f, (_Float16)16.f};
-            const f16x2 less_near = {(_Float16)-1032.f, (_Float16)-1032.f}, less_far = {(_Float16)-1152.f, (_Float16)-1152.f};
+            const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) qsum[gr] = less[gr] = 0.f;
-#pragma unroll
-            for (int k = 0; k < KK; ++k)
+            for (int k = 0; k < KK; ++k) {
+                u32x4 x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = w[k][i] & keep;
-                    const float f = i & 1 ? far : near;
-                    const f16x2 t = {(_Float16)(__uint_as_float(x << 16) * f), (_Float16)(__uint_as_float(x & 0xffff0000u) * f)};
-                    q16[k][2 * i] = t[0];
-                    q16[k][2 * i + 1] = t[1];
-                    qsum[32 * k / kKvGroup] = __builtin_amdgcn_fdot2(t, i & 1 ? sixteen : one, qsum[32 * k / kKvGroup], false);
-                    less[32 * k / kKvGroup] = __builtin_amdgcn_fdot2(t, i & 1 ? less_far : less_near, less[32 * k / kKvGroup], false);
+                    x[i] = (w[k][i] ^ sign) & keep;
+                    qsum[32 * k / kKvGroup] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)x[i]), one, qsum[32 * k / kKvGroup], false);
                 }
-#pragma unroll
-            for (int gr = 0; gr < NG; ++gr) less[gr] = quarters_sum(less[gr]);
-            kappa = fabsf(a.scale) * __uint_as_float((uint32_t)(127 - up) << 23);
+                q16[k] = __builtin_bit_cast(bf16x8, x);
+            }
         }
+        kappa = fabsf(a.scale);
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) qsum[gr] = quarters_sum(qsum[gr]);
+        for (int gr = 0; gr < NG; ++gr) {
+            qsum[gr] = quarters_sum(qsum[gr]);
+            less[gr] = F32 ? 0.f : -136.f * qsum[gr];
+        }
         slack = real ? kSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;       // kappa = 0: infinite as well, the maximum never has to move
         vhi = real ? (a.all ? len : min(pos + 1, len)) : 0;
         vlo = real ? (a.window > 0 ? max(pos - a.window + 1, 0) : 0) : 0;
@@ -549,7 +538,7 @@ struct attn_state {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], q32[k][i], c, 0, 0, 0);
                 } else {
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_near_far(word, masks), q16[k], c, 0, 0, 0);
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, codes_on(word, masks.near, masks.magic_bf16)), q16[k], c, 0, 0, 0);
                 }
             }
 #pragma unroll
@@ -639,7 +628,7 @@ struct attn_state {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(less8, ps, o[4 * gr + i], 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_near(r.v[gr][i], masks), ps, o[4 * gr + i], 0, 0, 0);
+                for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, codes_on(r.v[gr][i], masks.near, masks.magic)), ps, o[4 * gr + i], 0, 0, 0);
             }
         }
     }
