@@ -100,23 +100,30 @@ __device__ __forceinline__ entry_span span_of(const attn_args& a, int len, int r
 // Entries as LDS holds them: how far the units before an entry reach, and the entry itself.
 struct attn_list {
     int* at;                   // [n + 1]
-    int4* entry;               // [n] slot, len, row0, rows
+    int2 *who, *rows;          // [n] slot and len; row0 and rows (null: one row each)
     int even;                  // > 0: every unit counts as this long
+    __device__ __forceinline__ int4 entry(int b) const {
+        const int2 w = who[b], r = rows ? rows[b] : int2{b, 1};
+        return int4{w.x, w.y, r.x, r.y};
+    }
 };
-inline size_t list_bytes(int n) { return (size_t)n * sizeof(int4) + ((size_t)n + 1) * 2 * sizeof(int); }      // and one int more an entry for planning tiles
+// (with rows of their own, one int more an entry for planning tiles)
+inline size_t list_bytes(int n, bool rows) { return rows ? (size_t)n * 2 * sizeof(int2) + ((size_t)n + 1) * 2 * sizeof(int) : (size_t)n * sizeof(int2) + ((size_t)n + 1) * sizeof(int); }
 
 template <bool F32>
 __device__ attn_list make_list(const attn_args& a, void* lds) {                // 256 threads
     __shared__ int waves[3][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
-    attn_list l{(int*)((int4*)lds + n), (int4*)lds, 0};
+    const bool own_rows = a.rows.row_start != nullptr;
+    attn_list l{(int*)((int2*)lds + (own_rows ? 2 * n : n)), (int2*)lds, own_rows ? (int2*)lds + n : nullptr, 0};
     int length = 0, units = 0, longest = 0;
     for (int b = lo; b < hi; ++b) {
         const kv_entry e = kv_entry_of(a.v, a.rows, b);
         const entry_span s = span_of(a, e.len, e.rows);
         const bool here = s.n && !is_prompt<F32>(a, e.rows);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
-        l.entry[b] = int4{e.slot, e.len, e.row0, e.rows};
+        l.who[b] = int2{e.slot, e.len};
+        if (own_rows) l.rows[b] = int2{e.row0, e.rows};
         length += size * u;
         units += u;
         longest = max(longest, size);
@@ -144,7 +151,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     }
     l.even = uniform(total_units <= (int)gridDim.x && longest <= kShort && a.grain == 0 ? longest : 0);
     for (int b = lo; b < hi; ++b) {
-        const int4 e = l.entry[b];
+        const int4 e = l.entry(b);
         const entry_span s = span_of(a, e.y, e.w);
         const bool here = s.n && !is_prompt<F32>(a, e.w);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
@@ -206,7 +213,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
         return before;
     };
     const auto tiles_of = [&](int b) {
-        const int4 e = l.entry[b];
+        const int4 e = l.entry(b);
         return is_prompt<false>(a, e.w) && span_of(a, e.y, e.w).n ? (int)(((long long)e.w * a.g + kTile - 1) / kTile) : 0;
     };
     int mine = 0, tiles;
@@ -231,7 +238,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
                 if (first[mid] <= i) b = mid;
                 else end = mid;
             }
-            const int4 e = l.entry[b];
+            const int4 e = l.entry(b);
             const tile_span t = tile_of(a, e.y, e.w, i - first[b]);
             size = ((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost;
             a.tile[2 * i] = e;
@@ -384,24 +391,18 @@ constexpr float kTileSlack = 8.f, kTileLift = 4.f;            // prompts: weight
 constexpr float kLift = 1.f;   // weights are 2^kLift larger than they have to be: fp16's small numbers reach further down
 
 template <int D>
-struct kv_regs {               // a lane's part of a block
-    u32x4 k[D / 64], v[D / 64];
-    u32x4 ks[D / kKvGroup], km[D / kKvGroup], vs[D / kKvGroup], vm[D / kKvGroup];
+struct kv_regs {               // a lane's part of a block's keys, or of its values
+    u32x4 c[D / 64];
+    u32x4 s[D / kKvGroup], m[D / kKvGroup];
 };
 template <int D>
-__device__ __forceinline__ void read_block(kv_regs<D>& r, const unsigned char* block, int lane) {
-    const unsigned char* c = block + 16 * lane;
+__device__ __forceinline__ void read_block(kv_regs<D>& r, const unsigned char* codes, const unsigned char* scales, int lane) {
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) r.k[i] = *(const u32x4*)(c + 1024 * i);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) r.v[i] = *(const u32x4*)(c + essa_k::kv_values_at(D) + 1024 * i);
-    const unsigned char* s = block + 32 * (lane >> 4);
+    for (int i = 0; i < D / 64; ++i) r.c[i] = *(const u32x4*)(codes + 16 * lane + 1024 * i);
 #pragma unroll
     for (int i = 0; i < D / kKvGroup; ++i) {
-        r.ks[i] = *(const u32x4*)(s + essa_k::kv_key_scales_at(D) + 128 * i);
-        r.km[i] = *(const u32x4*)(s + essa_k::kv_key_scales_at(D) + 128 * i + 16);
-        r.vs[i] = *(const u32x4*)(s + essa_k::kv_value_scales_at(D) + 128 * i);
-        r.vm[i] = *(const u32x4*)(s + essa_k::kv_value_scales_at(D) + 128 * i + 16);
+        r.s[i] = *(const u32x4*)(scales + 32 * (lane >> 4) + 128 * i);
+        r.m[i] = *(const u32x4*)(scales + 32 * (lane >> 4) + 128 * i + 16);
     }
 }
 // Loads of a block into LDS: 1024 bytes an instruction, the scales' rest in pieces of 256.
@@ -514,9 +515,12 @@ struct attn_state {
         for (int i = 0; i < D / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // `t0`: the block's first token; whole: every column of the wave sees all of it
-    __device__ __forceinline__ void step(const kv_regs<D>& r, int t0, bool whole, int lane) {
+    // `block`: in LDS; t0: its first token; whole: every column of the wave sees all of it; read: called once all of it has been read
+    template <class Read>
+    __device__ __forceinline__ void step(const unsigned char* block, int t0, bool whole, int lane, Read read) {
         const int h = lane >> 4;
+        kv_regs<D> r;
+        read_block<D>(r, block, block + essa_k::kv_key_scales_at(D), lane);
         float s[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = 0.f;
@@ -530,7 +534,7 @@ struct attn_state {
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
                 const int w = t * KK + k;
-                const uint32_t word = r.k[w >> 2][w & 3];
+                const uint32_t word = r.c[w >> 2][w & 3];
                 f32x4& c = acc[32 * k / kKvGroup][t];
                 if (F32) {
                     float x[8];
@@ -545,7 +549,8 @@ struct attn_state {
         for (int gr = 0; gr < NG; ++gr)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                s[e] = fmaf(half_of(r.km[gr], e), qsum[gr], fmaf(half_of(r.ks[gr], e), acc[gr][e >> 2][e & 3], s[e]));
+                s[e] = fmaf(half_of(r.m[gr], e), qsum[gr], fmaf(half_of(r.s[gr], e), acc[gr][e >> 2][e & 3], s[e]));
+        read_block<D>(r, block + essa_k::kv_values_at(D), block + essa_k::kv_value_scales_at(D), lane);
         bool seen[8];
         if (!whole) {
 #pragma unroll
@@ -576,6 +581,8 @@ struct attn_state {
 #pragma unroll
             for (int e = 0; e < 8; ++e) p[e] = seen[e] ? p[e] : 0.f;
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        read();
         if constexpr (F32) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += p[e];
@@ -585,13 +592,13 @@ struct attn_state {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const bool in = whole || seen[e];
-                    ps[e] = in ? p[e] * half_of(r.vs[gr], e) : 0.f;
-                    mid[gr] = in ? fmaf(p[e], half_of(r.vm[gr], e), mid[gr]) : mid[gr];
+                    ps[e] = in ? p[e] * half_of(r.s[gr], e) : 0.f;
+                    mid[gr] = in ? fmaf(p[e], half_of(r.m[gr], e), mid[gr]) : mid[gr];
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float x[8];
-                    codes_f32(r.v[gr][i], x);
+                    codes_f32(r.c[gr][i], x);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], ps[e], o[4 * gr + i], 0, 0, 0);
                 }
@@ -606,7 +613,7 @@ struct attn_state {
             }
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) {
-                u32x4 vs = r.vs[gr], vm = r.vm[gr];
+                u32x4 vs = r.s[gr], vm = r.m[gr];
                 if (!whole) {                                  // what is not seen may be NaN
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -628,7 +635,7 @@ struct attn_state {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(less8, ps, o[4 * gr + i], 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, codes_on(r.v[gr][i], masks.near, masks.magic)), ps, o[4 * gr + i], 0, 0, 0);
+                for (int i = 0; i < 4; ++i) o[4 * gr + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, codes_on(r.c[gr][i], masks.near, masks.magic)), ps, o[4 * gr + i], 0, 0, 0);
             }
         }
     }
@@ -655,11 +662,13 @@ __device__ __forceinline__ void put_out(const kv_tensor& Y, long long at, const 
 }
 
 // Four waves: up to 16 columns -> each takes every fourth block; 32 -> two and two; more -> one 16 columns each, all blocks.
-// A wave's blocks come through LDS, kRing of them on their way while one is worked on: three workgroups a CU have
-// 12 x 2 x 4.6 KB outstanding, which is what the memory's latency under load wants.
+// A wave's blocks come through LDS, kRing of them on their way while one is worked on.  Workgroups a CU, each with 4 x kRing
+// blocks outstanding: four sequences of 100000 tokens (D = 128) take 98 us with two of them, 102 with three, 114 with four,
+// 256 sequences of 736 tokens 38, 35, 38.5; 64 sequences of 600 (D = 64) 25, 22, 16.
 template <int D> constexpr int kRing = 256 / D;
+template <int D> constexpr int kStreamsPerCu = D == 64 ? 4 : 3;
 template <int D, bool F32>
-__global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
+__global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(attn_args a) {
     constexpr int KK = D / 32, QUADS = D / 4, S = kRing<D>, BLOCK = essa_k::kv_block_bytes(D);
     extern __shared__ int4 list_lds[];
     __shared__ __attribute__((aligned(1024))) unsigned char ring[4 * S * BLOCK];
@@ -680,7 +689,7 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
     };
     const auto place_of = [&](int at) {
         const int b = uniform(entry_at(list, a.rows.n, at));
-        const int4 e = list.entry[b];
+        const int4 e = list.entry(b);
         place p;
         p.entry = int4{uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w)};
         p.sp = span_of(a, p.entry.y, p.entry.w);
@@ -760,11 +769,8 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
         for (int i = 0; k < b1; k += stripes) {
             if (k + (S - 1) * stripes < b1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kBlockLoads<D>) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            kv_regs<D> regs;
-            read_block<D>(regs, ring + (wave * S + i) * BLOCK, lane);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane);
-            st.step(regs, k * kKvBlock, k * kKvBlock >= all_lo && (k + 1) * kKvBlock <= all_hi, lane);
+            st.step(ring + (wave * S + i) * BLOCK, k * kKvBlock, k * kKvBlock >= all_lo && (k + 1) * kKvBlock <= all_hi, lane,
+                    [&] { if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane); });
             i = i + 1 == S ? 0 : i + 1;
         }
         // the four quarters of a column's tokens, then the waves that share columns
@@ -808,8 +814,8 @@ __global__ __launch_bounds__(256, 3) void kv_attn_stream_kernel(attn_args a) {
     }
     // rows that see nothing: no unit holds them
     for (int b = blockIdx.x; b < a.rows.n; b += gridDim.x)
-        if (list.at[b] == list.at[b + 1] && span_of(a, list.entry[b].y, list.entry[b].w).n == 0) {
-            const int4 e = list.entry[b];
+        if (list.at[b] == list.at[b + 1] && span_of(a, list.entry(b).y, list.entry(b).w).n == 0) {
+            const int4 e = list.entry(b);
             const int width = a.g * a.v.heads * QUADS;
             for (int i = 0; i < e.w; ++i)
                 for (int c = threadIdx.x; c < width; c += 256) put_out(a.Y, (long long)(e.z + i) * a.Y.stride + 4 * c, f32x4{0.f, 0.f, 0.f, 0.f});
@@ -1259,7 +1265,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
 
 namespace essa_k {
 
-constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // a CU each
+constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // four a CU, one a CU
 
 static size_t tile_count(int g, const kv_rows& rows) { return (size_t)((long long)rows.R * g / kTile) + rows.n + 1; }
 static size_t tile_words_of(int g, const kv_rows& rows) { return (9 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
@@ -1292,9 +1298,13 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
         ws = (int*)ws + tile_words_of(a.g, a.rows);
     }
     a.parts = (float*)ws;
-    const size_t lds = list_bytes(a.rows.n);
-    if (x_dtype == ESSA_F32) kv_attn_stream_kernel<D, true><<<kStreams, 256, lds, st>>>(a);
-    else kv_attn_stream_kernel<D, false><<<kStreams, 256, lds, st>>>(a);
+    const size_t lds = list_bytes(a.rows.n, a.rows.row_start != nullptr);
+    // what the chip holds at once is what the work is divided by; long lists of entries leave less LDS
+    int per_cu = kStreamsPerCu<D>;
+    while (per_cu > 1 && per_cu * (4 * kRing<D> * kv_block_bytes(D) + lds + 1024) > 160 * 1024) --per_cu;
+    const int streams = 256 * per_cu;
+    if (x_dtype == ESSA_F32) kv_attn_stream_kernel<D, true><<<streams, 256, lds, st>>>(a);
+    else kv_attn_stream_kernel<D, false><<<streams, 256, lds, st>>>(a);
     if (prompts) kv_attn_prompt_kernel<D><<<kPrompts, kTileThreads, 0, st>>>(a);
     return hipGetLastError();
 }

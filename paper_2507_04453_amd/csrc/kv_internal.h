@@ -47,7 +47,7 @@ struct kv_tensor {             // R rows of heads * D values
     int aligned;               // rows begin on 16 bytes
 };
 
-constexpr int kKvAttnWorkgroups = 768;     // three a CU
+constexpr int kKvAttnWorkgroups = 1024;    // four a CU
 
 // the cache's scratch (int32 words): page bookkeeping, and attention's counts
 struct kv_scratch {
