@@ -34,13 +34,27 @@ __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, 
     const bool mine = tok >= first && tok < last;
     const long long row = e.row0 + (t0 + tok - p0);
 
+    // everything that comes from memory is asked for at once: both rows, and the words that keep old tokens' codes
+    float rows_in[2][CH];
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
         const kv_tensor& X = side ? V : K;
-        float x[CH];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) x[i] = 0.f;
-        if (mine) kv_load<CH>(X, row * X.stride + (long long)head * D + part * CH, x);
+        for (int i = 0; i < CH; ++i) rows_in[side][i] = 0.f;
+        if (mine) kv_load<CH>(X, row * X.stride + (long long)head * D + part * CH, rows_in[side]);
+    }
+    // a single token touches one word of every channel; what lies in a block behind its last token does not matter
+    const bool one = last - first == 1;
+    uint32_t old[4 * D / 256];
+#pragma unroll
+    for (int k = 0; k < 4 * D / 256; ++k) {
+        const int i = threadIdx.x + 256 * k;
+        old[k] = first > 0 && (!one || i / D == kv_run(first)) ? *(const uint32_t*)(out + kv_value_word<D>(i / D, i % D)) : 0;
+    }
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        if (!__any(mine)) break;                               // eight tokens a wave: for a row a sequence three of four have nothing to do
+        float (&x)[CH] = rows_in[side];
         bool finite = true;
         float lo = 32768.f, hi = -32768.f;
 #pragma unroll
@@ -83,18 +97,23 @@ __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, 
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 4 * D; i += 256) {
-        const int h = i / D, c = i % D;
-        uint32_t w = 0, keep = 0;
 #pragma unroll
-        for (int el = 0; el < 8; ++el) {
-            const int t = (el & 3) + 16 * (el >> 2) + 4 * h;
-            if (t < first) keep |= 15u << kv_shift(el);
-            else if (t < last) w |= (uint32_t)codes[t][c] << kv_shift(el);
+    for (int k = 0; k < 4 * D / 256; ++k) {
+        const int i = threadIdx.x + 256 * k, h = i / D, c = i % D;
+        uint32_t w = 0, keep = 0;
+        if (one) {
+            if (h != kv_run(first)) continue;
+            keep = ~(15u << kv_shift(kv_element(first)));
+            w = (uint32_t)codes[first][c] << kv_shift(kv_element(first));
+        } else {
+#pragma unroll
+            for (int el = 0; el < 8; ++el) {
+                const int t = (el & 3) + 16 * (el >> 2) + 4 * h;
+                if (t < first) keep |= 15u << kv_shift(el);
+                else if (t < last) w |= (uint32_t)codes[t][c] << kv_shift(el);
+            }
         }
-        uint32_t* at = (uint32_t*)(out + kv_value_word<D>(h, c));
-        if (keep) w |= *at & keep;
-        *at = w;
+        *(uint32_t*)(out + kv_value_word<D>(h, c)) = w | (old[k] & keep);
     }
 }
 
