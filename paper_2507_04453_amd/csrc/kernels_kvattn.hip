@@ -80,10 +80,14 @@ struct attn_args {
     int tile_grain, tile_least;
 };
 constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
-// An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16): there a
-// block is unpacked once for 256 columns instead of once for 16.  At 65 columns and 4000 tokens the two kernels are even.
-template <bool F32>
-__device__ __forceinline__ bool is_prompt(const attn_args& a, int rows) { return !F32 && a.tiles && rows > 1 && (long long)rows * a.g > kColumns; }
+// An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16), where a block
+// is unpacked once for 256 columns instead of once for 16 -- unless all of the call is little work for the stream kernel
+// (kLittle, as its row of units would be long): tiles of 256 columns are then too few to fill the chip, or their parts too large to
+// join.  28 heads on 4 of 128, us, stream and prompt kernel: a prompt of 128 tokens 15 and 30 (length 1100), of 512 26 and 36
+// (4900); 256 rows behind 1744 tokens 51 and 85 (7700); 16 prompts of 128 33 and 32 (9000); 8 x 36 rows behind 8000 tokens
+// 115 and 112 (33000); 64 x 36 behind 264 56 and 44 (16000); 64 x 36 behind 2000 182 and 143 (70000).  Between 8000 and 30000
+// either may be ahead, by up to a third.
+constexpr int kLittle = 8192;
 
 struct entry_span {            // the blocks that an entry's rows see, and how many units of kColumns columns it has for each key head
     int lo, n, groups;
@@ -102,11 +106,13 @@ struct attn_list {
     int* at;                   // [n + 1]
     int2 *who, *rows;          // [n] slot and len; row0 and rows (null: one row each)
     int even;                  // > 0: every unit counts as this long
+    bool prompts;              // entries of many rows are the prompt kernel's
     __device__ __forceinline__ int4 entry(int b) const {
         const int2 w = who[b], r = rows ? rows[b] : int2{b, 1};
         return int4{w.x, w.y, r.x, r.y};
     }
 };
+__device__ __forceinline__ bool is_prompt(const attn_args& a, const attn_list& l, int rows) { return l.prompts && rows > 1 && (long long)rows * a.g > kColumns; }
 // (with rows of their own, one int more an entry for planning tiles)
 inline size_t list_bytes(int n, bool rows) { return rows ? (size_t)n * 2 * sizeof(int2) + ((size_t)n + 1) * 2 * sizeof(int) : (size_t)n * sizeof(int2) + ((size_t)n + 1) * sizeof(int); }
 
@@ -115,12 +121,25 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     __shared__ int waves[3][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
     const bool own_rows = a.rows.row_start != nullptr;
-    attn_list l{(int*)((int2*)lds + (own_rows ? 2 * n : n)), (int2*)lds, own_rows ? (int2*)lds + n : nullptr, 0};
+    attn_list l{(int*)((int2*)lds + (own_rows ? 2 * n : n)), (int2*)lds, own_rows ? (int2*)lds + n : nullptr, 0, false};
+    if (!F32 && a.tiles) {                                     // every workgroup finds the same
+        int work = 0;
+        for (int b = lo; b < hi; ++b) {
+            const kv_entry e = kv_entry_of(a.v, a.rows, b);
+            const entry_span s = span_of(a, e.len, e.rows);
+            if (s.n) work += (int)min((long long)s.groups * a.v.heads * (s.n + kUnitCost), (long long)kLittle + 1);
+        }
+        work = wave_scan(work, [](int x, int y) { return x + y; });
+        if ((threadIdx.x & 63) == 63) waves[0][threadIdx.x / 64] = work;
+        lds_barrier();
+        l.prompts = uniform(waves[0][0] + waves[0][1] + waves[0][2] + waves[0][3]) > kLittle;
+        lds_barrier();
+    }
     int length = 0, units = 0, longest = 0;
     for (int b = lo; b < hi; ++b) {
         const kv_entry e = kv_entry_of(a.v, a.rows, b);
         const entry_span s = span_of(a, e.len, e.rows);
-        const bool here = s.n && !is_prompt<F32>(a, e.rows);
+        const bool here = s.n && !is_prompt(a, l, e.rows);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.who[b] = int2{e.slot, e.len};
         if (own_rows) l.rows[b] = int2{e.row0, e.rows};
@@ -153,7 +172,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     for (int b = lo; b < hi; ++b) {
         const int4 e = l.entry(b);
         const entry_span s = span_of(a, e.y, e.w);
-        const bool here = s.n && !is_prompt<F32>(a, e.w);
+        const bool here = s.n && !is_prompt(a, l, e.w);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.at[b] = l.even ? units_at * l.even : length_at;
         length_at += size * u;
@@ -214,7 +233,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
     };
     const auto tiles_of = [&](int b) {
         const int4 e = l.entry(b);
-        return is_prompt<false>(a, e.w) && span_of(a, e.y, e.w).n ? (int)(((long long)e.w * a.g + kTile - 1) / kTile) : 0;
+        return is_prompt(a, l, e.w) && span_of(a, e.y, e.w).n ? (int)(((long long)e.w * a.g + kTile - 1) / kTile) : 0;
     };
     int mine = 0, tiles;
     for (int b = lo; b < hi; ++b) mine += tiles_of(b);
@@ -836,7 +855,6 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 // A NaN among the values must not reach columns that do not see it (0 times NaN): it is taken out and noted, and the
 // columns that see it are made NaN.
 // ---------------------------------------------------------------------------------------------
-typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
 constexpr int kTileThreads = 512;
 
 // N products with operands from LDS, some reads on their way in front of each (left alone, the compiler reads one operand
