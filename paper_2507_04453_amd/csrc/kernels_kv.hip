@@ -16,8 +16,13 @@ __device__ __forceinline__ __half half_of_single(float x) {
 // of 64 channels is 4 (D = 128) or 8 (D = 64) neighbouring lanes.  Keys go out as each thread has them (its channels are
 // whole words of its token); the words of values hold one channel of eight tokens and are put together through LDS, those
 // of a block that is not new from its first token on with the old tokens' codes kept.
-// Bound by launch and latency for a row or two a sequence, by the bytes of K and V for prompts.
-template <int D>
+// Bound by launch and latency for a row or two a sequence (one row to each of 256 sequences, 4 heads of 128: 4.8 us), by the
+// bytes of K and V for prompts (28339 rows, 8 heads of 128: 42 us, 3.5 TB/s).
+//
+// SINGLE: one row an entry, where the time is that of dependent loads: both rows and the words that keep old tokens' codes are asked for at
+// once, and waves without a token are spared the arithmetic (256 of them 7.0 -> 4.8 us).  With rows of their own the registers that
+// this takes cost more than it gives: 28339 rows, appended and read back, 67 -> 71 us.
+template <int D, bool SINGLE>
 __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, kv_tensor V, kv_rows rows) {
     constexpr int CH = D / 8, NG = D / kKvGroup;
     __shared__ unsigned char codes[kKvBlock][D + 4];
@@ -34,26 +39,25 @@ __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, 
     const bool mine = tok >= first && tok < last;
     const long long row = e.row0 + (t0 + tok - p0);
 
-    // everything that comes from memory is asked for at once: both rows, and the words that keep old tokens' codes
     float rows_in[2][CH];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
+    const auto load = [&](int side) {
         const kv_tensor& X = side ? V : K;
 #pragma unroll
         for (int i = 0; i < CH; ++i) rows_in[side][i] = 0.f;
         if (mine) kv_load<CH>(X, row * X.stride + (long long)head * D + part * CH, rows_in[side]);
-    }
+    };
+    const auto value_word = [&](int h, int c) { return (uint32_t*)(out + kv_value_word<D>(h, c)); };
     // a single token touches one word of every channel; what lies in a block behind its last token does not matter
-    const bool one = last - first == 1;
-    uint32_t old[4 * D / 256];
-#pragma unroll
-    for (int k = 0; k < 4 * D / 256; ++k) {
-        const int i = threadIdx.x + 256 * k;
-        old[k] = first > 0 && (!one || i / D == kv_run(first)) ? *(const uint32_t*)(out + kv_value_word<D>(i / D, i % D)) : 0;
+    uint32_t old = 0;
+    if constexpr (SINGLE) {
+        load(0);
+        load(1);
+        if (threadIdx.x < D && first > 0) old = *value_word(kv_run(first), threadIdx.x);
     }
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
-        if (!__any(mine)) break;                               // eight tokens a wave: for a row a sequence three of four have nothing to do
+        if constexpr (!SINGLE) load(side);
+        else if (!__any(mine)) break;                          // eight tokens a wave: three of four have nothing to do
         float (&x)[CH] = rows_in[side];
         bool finite = true;
         float lo = 32768.f, hi = -32768.f;
@@ -97,27 +101,30 @@ __global__ __launch_bounds__(256) void kv_append_kernel(kv_view v, kv_tensor K, 
         }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 4 * D / 256; ++k) {
-        const int i = threadIdx.x + 256 * k, h = i / D, c = i % D;
-        uint32_t w = 0, keep = 0;
-        if (one) {
-            if (h != kv_run(first)) continue;
-            keep = ~(15u << kv_shift(kv_element(first)));
-            w = (uint32_t)codes[first][c] << kv_shift(kv_element(first));
-        } else {
-#pragma unroll
-            for (int el = 0; el < 8; ++el) {
-                const int t = (el & 3) + 16 * (el >> 2) + 4 * h;
-                if (t < first) keep |= 15u << kv_shift(el);
-                else if (t < last) w |= (uint32_t)codes[t][c] << kv_shift(el);
-            }
+    if constexpr (SINGLE) {
+        if (threadIdx.x < D) {
+            const int shift = kv_shift(kv_element(first));
+            *value_word(kv_run(first), threadIdx.x) = (old & ~(15u << shift)) | (uint32_t)codes[first][threadIdx.x] << shift;
         }
-        *(uint32_t*)(out + kv_value_word<D>(h, c)) = w | (old[k] & keep);
+        return;
+    }
+    for (int i = threadIdx.x; i < 4 * D; i += 256) {
+        const int h = i / D, c = i % D;
+        uint32_t w = 0, keep = 0;
+#pragma unroll
+        for (int el = 0; el < 8; ++el) {
+            const int t = (el & 3) + 16 * (el >> 2) + 4 * h;
+            if (t < first) keep |= 15u << kv_shift(el);
+            else if (t < last) w |= (uint32_t)codes[t][c] << kv_shift(el);
+        }
+        if (keep) w |= *value_word(h, c) & keep;
+        *value_word(h, c) = w;
     }
 }
 
-// The reverse: same split, the values' words of a block gathered through LDS.
+// The reverse, x = m + s q, rounded once to the output's type: same split, the values' words of a block gathered through LDS.
+// Bound by the bytes of K and V that go out, near four times what comes in.  28339 rows, 8 heads of
+// 128: 29 us, 5.2 TB/s.
 template <int D>
 __global__ __launch_bounds__(256) void kv_read_kernel(kv_view v, kv_tensor K, kv_tensor V, kv_rows rows) {
     constexpr int CH = D / 8, NG = D / kKvGroup;
@@ -168,8 +175,8 @@ namespace essa_k {
 
 hipError_t kv_append(hipStream_t st, const kv_view& v, int D, const kv_tensor& K, const kv_tensor& V, const kv_rows& rows) {
     const dim3 grid(kv_places(rows), v.heads);
-    if (D == 64) kv_append_kernel<64><<<grid, 256, 0, st>>>(v, K, V, rows);
-    else kv_append_kernel<128><<<grid, 256, 0, st>>>(v, K, V, rows);
+    if (rows.row_start) (D == 64 ? kv_append_kernel<64, false> : kv_append_kernel<128, false>)<<<grid, 256, 0, st>>>(v, K, V, rows);
+    else (D == 64 ? kv_append_kernel<64, true> : kv_append_kernel<128, true>)<<<grid, 256, 0, st>>>(v, K, V, rows);
     return hipGetLastError();
 }
 
