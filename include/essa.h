@@ -457,8 +457,10 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
  * of the sequence.  A row that sees no token gives zeros.  What the row does not see has no part in it, NaN or not; a row
  * of Q that holds an Inf or a NaN gives a row of NaN, a NaN in a K or V that it sees a NaN in that head.
  *   Q  DEVICE [R] rows of n_q_heads * head_dim values of x_dtype at q_stride * i;  Y likewise, y_dtype, y_stride
- * Arithmetic: bf16 Q -> products on the fp16 MFMA with fp32 accumulation, softmax statistics in fp32; fp32 Q -> fp32
- * throughout. */
+ * Arithmetic: sums and softmax statistics in fp32.  bf16 Q: keys meet the queries on the bf16 MFMA with their codes exact,
+ * weights and weights times scales are rounded to fp16; in calls of much work, entries with more than 64 pairs (row, query head) of a key head
+ * have K, V and the weights rounded to fp16 instead.  fp32 Q: fp32 throughout.  Equal calls give equal bits.
+ * The first call, and one larger than all before it, may allocate scratch (ESSA_ERR_STATE while a graph is recorded or alive). */
 #define ESSA_KV_ALL 0x1u
 essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
                               const essa_kv_batch* batch, float scale, int window, uint32_t flags, void* Y, int64_t y_stride, int y_dtype);

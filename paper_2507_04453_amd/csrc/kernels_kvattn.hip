@@ -684,6 +684,9 @@ __device__ __forceinline__ void put_out(const kv_tensor& Y, long long at, const 
 // A wave's blocks come through LDS, kRing of them on their way while one is worked on.  Workgroups a CU, each with 4 x kRing
 // blocks outstanding: four sequences of 100000 tokens (D = 128) take 98 us with two of them, 102 with three, 114 with four,
 // 256 sequences of 736 tokens 38, 35, 38.5; 64 sequences of 600 (D = 64) 25, 22, 16.
+// Long or many sequences are bound by memory: 4 x 100000 tokens of 8 heads 102 us (4.5 TB/s), 64 x 4096 60.5 us (5.0 TB/s).  A call
+// of little work is bound by what a workgroup does before its first block (list 4000 cycles, boundaries 4600, set-up 2000,
+// first loads 3600): 9.4 us for one sequence of 416 tokens.
 template <int D> constexpr int kRing = 256 / D;
 template <int D> constexpr int kStreamsPerCu = D == 64 ? 4 : 3;
 template <int D, bool F32>
@@ -852,6 +855,8 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 // The two waves of a SIMD take turns, a barrier between them: while one has the matrix cores (the values of its last stage,
 // the scores of its next) the other has the vector ALU (the weights of its stage, its share of unpacking a stage to come).
 // Left to themselves both did the same at the same time, and the time was the sum of the two.
+// Bound by issue: a turn takes about 2000 cycles, of which the matrix cores work 1024.  A prompt of 8192 rows (28 heads on 4 of
+// 128) 554 us, 869 TFLOP/s; four times 512 rows behind 30000 tokens (40 on 8) 1289 us, 967 TFLOP/s.
 // A NaN among the values must not reach columns that do not see it (0 times NaN): it is taken out and noted, and the
 // columns that see it are made NaN.
 // ---------------------------------------------------------------------------------------------
