@@ -458,7 +458,8 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
  * of Q that holds an Inf or a NaN gives a row of NaN, a NaN in a K or V that it sees a NaN in that head.
  *   Q  DEVICE [R] rows of n_q_heads * head_dim values of x_dtype at q_stride * i;  Y likewise, y_dtype, y_stride
  * Arithmetic: sums and softmax statistics in fp32.  bf16 Q: keys meet the queries on the bf16 MFMA with their codes exact,
- * weights and weights times scales are rounded to fp16; in calls of much work, entries with more than 64 pairs (row, query head) of a key head
+ * weights and weights times scales are rounded to fp16 (with the largest weight at 2^13 or more and scales brought below 1, so that
+ * values of any size from 1e-6 up keep its 11 bits); in calls of much work, entries with more than 64 pairs (row, query head) of a key head
  * have K, V and the weights rounded to fp16 instead.  fp32 Q: fp32 throughout.  Equal calls give equal bits.
  * The first call, and one larger than all before it, may allocate scratch (ESSA_ERR_STATE while a graph is recorded or alive). */
 #define ESSA_KV_ALL 0x1u

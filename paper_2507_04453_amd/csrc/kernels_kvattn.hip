@@ -402,12 +402,18 @@ __device__ __forceinline__ void load_raw(const kv_tensor& Q, long long at, uint3
 //   score = sum_group s <q, c - 8> + m sum q,      O = sum_group (p s) (c - 8) + sum p m.
 // bf16 queries: keys on the bf16 MFMA, every product exact; weights and weights times scales in fp16; sums in fp32.  fp32
 // queries: the same on the fp32 MFMA, with c - 8 as operands.
-// The running maximum moves only when a score passes it by 4 (in the exponent of 2), which after the first blocks is rare:
-// weights stay below 2^3 and times a scale (at most 4370) below the range of fp16.
+// The running maximum moves only when a score passes it by kSlack (in the exponent of 2), which after the first blocks is rare:
+// weights stay below 2^(kLift + kSlack) = 2^15.
+// bf16 queries: the scales of values are anything from 2^-24 to 4370, and a weight times a scale has to fit into fp16 at either
+// end.  Below 1 a scale is what it is: the largest weight is between 2^13 and 2^15, so products stay below 2^15, and 2^-25, what a
+// product may lose to fp16's lower end, is 2^-38 of the largest weight with a scale of 1, 2^-20 of it with one of 2^-18 (values
+// near 1e-5).  Where a wave has seen a scale of 1 or more the group's are multiplied by the power of two that brings all below 1; it moves,
+// like the maximum, when a larger scale comes, and comes off in fp32 after the last block.
 // ---------------------------------------------------------------------------------------------
 constexpr float kSlack = 2.f;  // what a score may pass the running maximum by, as an exponent of 2
 constexpr float kTileSlack = 8.f, kTileLift = 4.f;            // prompts: weights alone have to fit into fp16
-constexpr float kLift = 1.f;   // weights are 2^kLift larger than they have to be: fp16's small numbers reach further down
+constexpr float kLift = 13.f;  // weights are 2^kLift larger than they have to be: fp16's small numbers reach further down
+constexpr int kScaleOne = 14;  // exponent field of fp16 just below 1
 
 template <int D>
 struct kv_regs {               // a lane's part of a block's keys, or of its values
@@ -470,7 +476,8 @@ struct attn_state {
     float top;                 // running maximum, in units of the score
     float down;                // kLift - top * kappa
     float sum, mid[NG];        // this lane's tokens' share of sum p and sum p m
-    f32x4 o[D / 16];           // channel 16 i + 4 (lane / 16) + r
+    f32x4 o[D / 16];           // channel 16 i + 4 (lane / 16) + r; bf16: times what the group's scales are times
+    int big[NG];               // bf16: exponent field of the largest scale of values so far, kScaleOne at least; the same in every lane
 
     // w: the lane's channels 32 k + 8 (lane / 16) .. + 7 as they are in memory; pos: position of the column's row; real: the column exists
     static constexpr int RAW = F32 ? 8 : 4;                    // words of 8 channels
@@ -529,9 +536,37 @@ struct attn_state {
         down = kLift;
         sum = real && !finite && vlo < vhi ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
 #pragma unroll
-        for (int gr = 0; gr < NG; ++gr) mid[gr] = 0.f;
+        for (int gr = 0; gr < NG; ++gr) {
+            mid[gr] = 0.f;
+            big[gr] = kScaleOne;
+        }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // What comes off again: 2^(big - kScaleOne).
+    __device__ __forceinline__ float scale_unlift(int gr) const { return F32 ? 1.f : __uint_as_float((uint32_t)(127 - kScaleOne + big[gr]) << 23); }
+    // A group's scales (vs: 0 where this lane's column does not see the token) as they meet the weights.
+    __device__ __forceinline__ void lift_scales(int gr, u32x4& vs) {
+        typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, (uint32_t)vs[i]));
+        if (__any(max((int)most[0], (int)most[1]) >> 10 > big[gr])) {
+            int e = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int x = (vs[i >> 1] >> (16 * (i & 1)) & 0xffffu) >> 10;
+                e = max(e, x < 31 ? x : 0);                    // a NaN stays one whatever it is times
+            }
+            e = max(__builtin_amdgcn_readlane(wave_scan(e, [](int x, int y) { return max(x, y); }), 63), big[gr]);
+            const float f = __uint_as_float((uint32_t)(127 + big[gr] - e) << 23);
+            big[gr] = e;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[4 * gr + i] *= f;
+        }
+        const f16x2 lift = as_f16((uint32_t)(kScaleOne + 15 - big[gr]) * 0x04000400u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vs[i] = __builtin_bit_cast(uint32_t, as_f16(vs[i]) * lift);
     }
 
     // `block`: in LDS; t0: its first token; whole: every column of the wave sees all of it; read: called once all of it has been read
@@ -630,17 +665,34 @@ struct attn_state {
                 p2[i] = f16x2{(_Float16)p[2 * i], (_Float16)p[2 * i + 1]};
                 sum = __builtin_amdgcn_fdot2(p2[i], one, sum, false);
             }
+            if (!whole) {                                      // what is not seen may be NaN
 #pragma unroll
-            for (int gr = 0; gr < NG; ++gr) {
-                u32x4 vs = r.s[gr], vm = r.m[gr];
-                if (!whole) {                                  // what is not seen may be NaN
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t in = (seen[2 * i] ? 0xffffu : 0u) | (seen[2 * i + 1] ? 0xffff0000u : 0u);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t in = (seen[2 * i] ? 0xffffu : 0u) | (seen[2 * i + 1] ? 0xffff0000u : 0u);
-                        vs[i] &= in;
-                        vm[i] &= in;
+                    for (int gr = 0; gr < NG; ++gr) {
+                        r.s[gr][i] &= in;
+                        r.m[gr][i] &= in;
                     }
                 }
+            }
+            typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+            const u16x2 below_one = {0x3bff, 0x3bff};          // scales are >= 0, so ordered as their bits
+            u16x2 most = below_one;
+            bool ordinary = true;
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, (uint32_t)r.s[gr][i]));
+                ordinary = ordinary && big[gr] == kScaleOne;
+            }
+            if (!ordinary || __any(__builtin_bit_cast(uint32_t, most) != 0x3bff3bffu)) {
+#pragma unroll
+                for (int gr = 0; gr < NG; ++gr) lift_scales(gr, r.s[gr]);
+            }
+#pragma unroll
+            for (int gr = 0; gr < NG; ++gr) {
+                const u32x4 vs = r.s[gr], vm = r.m[gr];
                 f16x8 ps;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -802,7 +854,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         const float top2 = st.top > -kFar ? st.top * st.kappa : -kFar;         // as an exponent of 2
         lds_barrier();                                         // all blocks have been read
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *(f32x4*)&merged[wave][lane & 15][16 * i + 4 * h] = st.o[i] + st.mid[i / 4];
+        for (int i = 0; i < D / 16; ++i) *(f32x4*)&merged[wave][lane & 15][16 * i + 4 * h] = st.o[i] * st.scale_unlift(i / 4) + st.mid[i / 4];
         if (h == 0) {
             wsum[wave][lane] = st.sum;
             wtop[wave][lane] = top2;
