@@ -406,7 +406,9 @@ void essa_kv_destroy(essa_kv* kv);
  * row_start[b] .. row_start[b + 1] - 1 of the R rows, which are the LAST ones of the sequence: row j of its c rows is the
  * token at position len - c + j.  row_start = NULL: one row an entry (R = n).  A negative seqs[b] is skipped, so the
  * `served` of a call below can be passed on as it is; so is one past max_seqs.  The sequences of a call are distinct and
- * row_start ascends from 0 to R (trusted; entries out of [0, R] are brought into it). */
+ * row_start ascends from 0 to R.  This is not reported, but nothing outside of the rows and the cache is touched where it does not
+ * hold: entries out of [0, R] are brought into it, one that ends before it begins has no rows, what two entries both name is written by
+ * either, and attention does nothing if the entries together have more than R rows. */
 typedef struct essa_kv_batch {
     const int32_t* seqs;      /* DEVICE int32 [n]             */
     const int32_t* row_start; /* DEVICE int32 [n + 1] or NULL */
