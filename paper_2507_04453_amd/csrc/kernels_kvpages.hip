@@ -93,9 +93,9 @@ __global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len,
 
 struct pages_view {
     int32_t *table, *len, *refs;
-    int page_tokens, n_pages, max_seqs, max_pages;
+    int page_tokens, n_pages, max_seqs, max_pages, max_len;
     kv_scratch s;
-    __device__ int length(int slot) const { return min(max(len[slot], 0), max_pages * page_tokens); }
+    __device__ int length(int slot) const { return min(max(len[slot], 0), max_len); }
     __device__ int pages(int tokens) const { return (int)(((unsigned)tokens + page_tokens - 1) / page_tokens); }
     __device__ int page(int slot, int f) const { return (int)min((unsigned)table[(size_t)slot * max_pages + f], (unsigned)n_pages - 1u); }
 };
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void kv_compact_move_kernel(pages_view v, unsi
 
 pages_view view_of(const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
-    return {d.table, d.len, d.refs, d.page_tokens, d.n_pages, d.max_seqs, d.max_pages, essa_k::kv_scratch_of(kv)};
+    return {d.table, d.len, d.refs, d.page_tokens, d.n_pages, d.max_seqs, d.max_pages, essa_k::kv_max_len(d), essa_k::kv_scratch_of(kv)};
 }
 
 }  // namespace

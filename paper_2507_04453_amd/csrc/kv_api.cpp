@@ -142,6 +142,7 @@ static essa_k::kv_view view_of(const essa_kv* kv, int layer) {
     v.n_pages = d.n_pages;
     v.max_seqs = d.max_seqs;
     v.max_pages = d.max_pages;
+    v.max_len = essa_k::kv_max_len(d);
     return v;
 }
 static essa_k::kv_rows rows_of(const essa_kv_batch* b) { return {b->seqs, b->row_start, b->n, b->R}; }

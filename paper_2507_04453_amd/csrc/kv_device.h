@@ -12,7 +12,7 @@ using essa_k::kv_tensor;
 using essa_k::kv_view;
 
 // Entry b of a call: its sequence, its rows, and the positions that they are.  Whatever the arrays hold, rows stay in
-// [0, R], positions below max_pages pages.
+// [0, R], positions below max_len.
 struct kv_entry {
     int slot;                  // -1: skipped
     int row0, rows;
@@ -30,7 +30,7 @@ __device__ __forceinline__ kv_entry kv_entry_of(const kv_view& v, const kv_rows&
         e.row0 = b;
         e.rows = 1;
     }
-    e.len = e.slot < 0 ? 0 : min(max(v.len[e.slot], 0), (v.max_pages << v.page_shift) * kKvBlock);
+    e.len = e.slot < 0 ? 0 : min(max(v.len[e.slot], 0), v.max_len);
     return e;
 }
 

@@ -34,6 +34,7 @@ struct kv_view {
     const int32_t* len;
     long long page_bytes;
     int heads, page_shift, n_pages, max_seqs, max_pages;
+    int max_len;               // tokens that a sequence can have: of max_pages pages, and of all that there are; 2^28 at most
 };
 struct kv_rows {
     const int32_t* seqs;
@@ -57,6 +58,7 @@ struct kv_scratch {
     int32_t* count;            // [4]
     int32_t* done;             // [2 kKvAttnWorkgroups] attention's counts of finished parts, 0 between calls
 };
+inline int kv_max_len(const essa_kv_desc& d) { return (d.max_pages < d.n_pages ? d.max_pages : d.n_pages) * d.page_tokens; }
 size_t kv_scratch_words(const essa_kv_desc& d);
 kv_scratch kv_scratch_of(const essa_kv* kv);
 
