@@ -68,7 +68,7 @@ struct attn_args {
     int g;                     // query heads on a key head
     unsigned g_inverse;        // ceil(2^32 / g), for numbers below 2^32 / g
     float scale;               // times log2(e)
-    int window, all;
+    int window, all;           // window: 0 or below max_len
     int grain;
     int* done;                 // [2 workgroups] see join; 0 between calls
     float* parts;              // [2 workgroups][kColumns][D + 4]: sum of a column's weights, their largest exponent, -, -, weighted values
@@ -1414,7 +1414,7 @@ hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor
     a.g = q_heads / v.heads;
     a.g_inverse = (unsigned)((((unsigned long long)1 << 32) + a.g - 1) / a.g);
     a.scale = scale * 1.44269504088896340736f;
-    a.window = window;
+    a.window = window < v.max_len ? window : 0;               // what reaches past every token is none; so positions less a window stay ints
     a.all = all;
     a.done = done;
     return D == 64 ? run<64>(st, a, ws, Q.dtype) : run<128>(st, a, ws, Q.dtype);
