@@ -112,7 +112,7 @@ struct attn_list {
         return int4{w.x, w.y, r.x, r.y};
     }
 };
-__device__ __forceinline__ bool is_prompt(const attn_args& a, const attn_list& l, int rows) { return l.prompts && rows > 1 && (long long)rows * a.g > kColumns; }
+__device__ __forceinline__ bool is_prompt(const attn_args& a, const attn_list& l, int rows) { return l.prompts && rows > 1 && rows * a.g > kColumns; }
 // (with rows of their own, one int more an entry for planning tiles)
 inline size_t list_bytes(int n, bool rows) { return rows ? (size_t)n * 2 * sizeof(int2) + ((size_t)n + 1) * 2 * sizeof(int) : (size_t)n * sizeof(int2) + ((size_t)n + 1) * sizeof(int); }
 
@@ -223,7 +223,7 @@ struct tile_span {
 __device__ __forceinline__ tile_span tile_of(const attn_args& a, int len, int rows, int which) {
     tile_span t;
     const int c0 = which * kTile;
-    t.columns = (int)min((long long)rows * a.g - c0, (long long)kTile);
+    t.columns = min(rows * a.g - c0, kTile);                   // R rows of q_heads are below 2^31
     const int first = len - rows + c0 / a.g, last = len - rows + (c0 + t.columns - 1) / a.g;      // positions
     const int lo = a.window > 0 ? max(first - a.window + 1, 0) : 0, hi = a.all ? len : min(last + 1, len);
     t.lo = lo / kStage;
@@ -252,7 +252,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
     };
     const auto tiles_of = [&](int b) {
         const int4 e = l.entry(b);
-        return is_prompt(a, l, e.w) && span_of(a, e.y, e.w).n ? (int)(((long long)e.w * a.g + kTile - 1) / kTile) : 0;
+        return is_prompt(a, l, e.w) && span_of(a, e.y, e.w).n ? (int)(((unsigned)(e.w * a.g) + kTile - 1) / kTile) : 0;
     };
     int mine = 0, tiles;
     for (int b = lo; b < hi; ++b) mine += tiles_of(b);
@@ -1025,18 +1025,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
         at = unit_at + size;
         const bool begins = from == 0, complete = begins && to == grains;
         const int first = tile_lo + (from << a.tile_grain), stop = tile_lo + min(to << a.tile_grain, tile_n);
-        const int c0 = which * kTile, columns = (int)min((long long)rows * a.g - c0, (long long)kTile), j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
+        const int c0 = which * kTile, columns = min(rows * a.g - c0, kTile), j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
         // this wave's columns
         const int column = 32 * wave + l;
         const bool real = column < columns;
         const int x = r0 + (real ? column : 0), j = over_g(x), r = x - j * a.g, pos = len - rows + j0 + j;
         const int vhi = real ? (a.all ? len : min(pos + 1, len)) : 0, vlo = real && a.window > 0 ? max(pos - a.window + 1, 0) : 0;
-        int some_lo = 0x7fffffff, some_hi = 0, all_lo = 0, all_hi = 0x7fffffff;
+        int all_lo = 0, all_hi = 0x7fffffff;                   // what all of them see
         if (32 * wave < columns) {
             const int pos0 = len - rows + j0 + over_g(r0 + 32 * wave), pos1 = len - rows + j0 + over_g(r0 + min(32 * wave + 31, columns - 1));
-            some_lo = a.window > 0 ? max(pos0 - a.window + 1, 0) : 0;
             all_lo = a.window > 0 ? max(pos1 - a.window + 1, 0) : 0;
-            some_hi = a.all ? len : min(pos1 + 1, len);
             all_hi = a.all ? len : min(pos0 + 1, len);
         }
         // a thread's words of a stage (its block of the two; past the end the last one's again)
