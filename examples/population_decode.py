@@ -43,10 +43,12 @@ class Model:
             self.sigma.append(sigmas)
 
     def buffers(self, rows):
-        """Activations of a call of so many rows."""
-        new = lambda width: torch.empty(rows, width, device="cuda", dtype=torch.bfloat16)
+        """Activations of a call of so many rows, with everything that a step computes on the way: a recorded step writes where it wrote
+        when it was recorded, so nothing of it may be memory that somebody else is given later."""
+        new = lambda width, dtype=torch.bfloat16: torch.empty(rows, width, device="cuda", dtype=dtype)
         return {"x": new(self.hidden), "h": new(self.hidden), "q": new(self.hidden), "k": new(self.kv_heads * self.head_dim),
-                "v": new(self.kv_heads * self.head_dim), "a": new(self.hidden), "o": new(self.hidden)}
+                "v": new(self.kv_heads * self.head_dim), "a": new(self.hidden), "o": new(self.hidden),
+                "x32": new(self.hidden, torch.float32), "square": new(self.hidden, torch.float32), "norm": new(1, torch.float32)}
 
     def groups(self, buf, row2cand):
         """The marshalled projections of every layer: q, k and v together, then o."""
@@ -57,15 +59,18 @@ class Model:
         return out
 
     def forward(self, kv, buf, groups, batch):
-        """x <- x + o(attention(q, cache with k and v)) for every layer; the cache has room for the rows already."""
+        """x <- x + o(attention(q, cache with k and v)) for every layer; the cache has room for the rows already.  Allocates nothing."""
+        x32, norm = buf["x32"], buf["norm"]
         for l, (qkv, o) in enumerate(groups):
-            x = buf["x"].float()
-            buf["h"].copy_(x * torch.rsqrt(x.square().mean(1, keepdim=True) + 1e-6))
+            x32.copy_(buf["x"])
+            torch.mean(torch.mul(x32, x32, out=buf["square"]), 1, keepdim=True, out=norm)
+            norm.add_(1e-6).rsqrt_()
+            buf["h"].copy_(x32.mul_(norm))
             essa.essa_svdlora_forward_group(self.ctx, qkv)
             essa.essa_kv_append(self.ctx, kv, l, buf["k"], buf["v"], batch)
             essa.essa_kv_attention(self.ctx, kv, l, buf["q"], buf["a"], batch, scale=0.02 / math.sqrt(self.head_dim))
             essa.essa_svdlora_forward_group(self.ctx, o)
-            buf["x"] += 0.05 * buf["o"]
+            buf["x"] += buf["o"].mul_(0.05)
 
 
 def run(candidates=4, samples=4, layers=2, hidden=3584, kv_width=512, rank=16, head_dim=128, prompt=200, steps=48, record=True, quiet=False):
