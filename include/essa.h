@@ -459,6 +459,7 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
  * of the sequence.  A row that sees no token gives zeros.  What the row does not see has no part in it, NaN or not; a row
  * of Q that holds an Inf or a NaN gives a row of NaN, a NaN in a K or V that it sees a NaN in that head.
  *   Q  DEVICE [R] rows of n_q_heads * head_dim values of x_dtype at q_stride * i;  Y likewise, y_dtype, y_stride
+ *   scale  finite, and so is its product with log2(e)
  * Arithmetic: sums and softmax statistics in fp32.  bf16 Q: keys meet the queries on the bf16 MFMA with their codes exact,
  * weights and weights times scales are rounded to fp16 (with the largest weight at 2^13 or more and scales brought below 1, so that
  * values of any size from 1e-6 up keep its 11 bits); in calls of much work, entries with more than 64 pairs (row, query head) of a key head

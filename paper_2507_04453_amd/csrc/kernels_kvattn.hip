@@ -1402,7 +1402,7 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     return hipGetLastError();
 }
 
-hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale,
+hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale2,
                         int window, bool all, int32_t* done, void* ws) {
     attn_args a{};
     a.v = v;
@@ -1411,7 +1411,7 @@ hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor
     a.rows = rows;
     a.g = q_heads / v.heads;
     a.g_inverse = (unsigned)((((unsigned long long)1 << 32) + a.g - 1) / a.g);
-    a.scale = scale * 1.44269504088896340736f;
+    a.scale = scale2;
     a.window = window < v.max_len ? window : 0;               // what reaches past every token is none; so positions less a window stay ints
     a.all = all;
     a.done = done;

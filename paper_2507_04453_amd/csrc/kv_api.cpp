@@ -185,7 +185,8 @@ extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int l
     if (flags & ~ESSA_KV_ALL) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
     if (window < 0 || (window > 0 && (flags & ESSA_KV_ALL)))
         return essa_fail(ESSA_ERR_INVALID_ARG, "%s: window=%d%s", who, window, window < 0 ? "" : " together with ESSA_KV_ALL");
-    if (!(scale - scale == 0.0f)) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: scale is not finite", who);
+    const float scale2 = scale * essa_k::kLog2e;               // what the kernels take: exponents of 2
+    if (!(scale2 - scale2 == 0.0f)) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: scale=%g, it and its product with log2(e) have to be finite", who, (double)scale);
     if (batch->R == 0) return ESSA_OK;
     const int64_t width = (int64_t)n_q_heads * kv->d.head_dim;
     if (batch->R * (int64_t)n_q_heads >= ((int64_t)1 << 31)) return essa_fail(ESSA_ERR_SHAPE, "%s: R=%d rows of %d heads", who, batch->R, n_q_heads);
@@ -196,7 +197,7 @@ extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int l
     const essa_k::kv_view v = view_of(kv, layer);
     const essa_k::kv_rows rows = rows_of(batch);
     ESSA_TRY(essa_ws_reserve(ctx, essa_k::kv_attention_bytes(v, kv->d.head_dim, n_q_heads, rows, x_dtype)));
-    ESSA_HIP(essa_k::kv_attention(ctx->stream, v, kv->d.head_dim, q, y, n_q_heads, rows, scale, window, (flags & ESSA_KV_ALL) != 0,
+    ESSA_HIP(essa_k::kv_attention(ctx->stream, v, kv->d.head_dim, q, y, n_q_heads, rows, scale2, window, (flags & ESSA_KV_ALL) != 0,
                                   essa_k::kv_scratch_of(kv).done, ctx->ws));
     return ESSA_OK;
 }

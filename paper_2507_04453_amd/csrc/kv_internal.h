@@ -48,6 +48,7 @@ struct kv_tensor {             // R rows of heads * D values
     int aligned;               // rows begin on 16 bytes
 };
 
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kKvAttnWorkgroups = 1024;    // four a CU
 
 // the cache's scratch (int32 words): page bookkeeping, and attention's counts
@@ -71,6 +72,6 @@ hipError_t kv_append(hipStream_t st, const kv_view& v, int D, const kv_tensor& K
 hipError_t kv_read(hipStream_t st, const kv_view& v, int D, const kv_tensor& K, const kv_tensor& V, const kv_rows& rows);
 
 size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& rows, int x_dtype);
-hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale,
+hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale2 /*times log2(e)*/,
                         int window, bool all, int32_t* done, void* ws);
 }  // namespace essa_k
