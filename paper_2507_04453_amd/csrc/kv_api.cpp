@@ -39,7 +39,6 @@ extern "C" essa_status essa_kv_create(essa_ctx* ctx, const essa_kv_desc* d, essa
     if (!kv) return essa_fail(ESSA_ERR_OOM, "essa_kv_create: out of host memory");
     kv->ctx = ctx;
     kv->device = ctx->device;
-    kv->stream = ctx->stream;
     kv->d = *d;
     while ((essa_k::kKvBlock << kv->page_shift) < d->page_tokens) ++kv->page_shift;
     const size_t bytes = essa_k::kv_scratch_words(*d) * sizeof(int32_t);

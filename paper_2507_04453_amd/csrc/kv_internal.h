@@ -5,7 +5,6 @@
 struct essa_kv {
     essa_ctx* ctx = nullptr;   // identity check only; never dereferenced after creation
     int device = 0;
-    hipStream_t stream = nullptr;
     essa_kv_desc d{};
     int page_shift = 0;        // log2(page_tokens / 32)
     int32_t* scratch = nullptr;// page bookkeeping: see kv_scratch
