@@ -760,7 +760,6 @@ __device__ __forceinline__ void put_out(const kv_tensor& Y, long long at, const 
 // first loads 3600): 9.4 us for one sequence of 416 tokens.
 template <int D> constexpr int kRing = 256 / D;
 template <int D> constexpr int kStreamsPerCu = D == 64 ? 4 : 3;
-static_assert(256 * kStreamsPerCu<64> <= essa_k::kKvAttnWorkgroups, "");
 template <int D, bool F32, bool OWN_ROWS>
 __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(attn_args a) {
     constexpr int KK = D / 32, QUADS = D / 4, S = kRing<D>, BLOCK = essa_k::kv_block_bytes(D);
@@ -1358,7 +1357,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
 
 namespace essa_k {
 
-constexpr int kCus = 256, kPrompts = kCus;
+constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // four a CU, one a CU
 
 static size_t tile_count(int g, const kv_rows& rows) { return (size_t)((long long)rows.R * g / kTile) + rows.n + 1; }
 static size_t tile_words_of(int g, const kv_rows& rows) { return (9 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
@@ -1368,7 +1367,7 @@ static bool may_have_prompts(int x_dtype, int g, const kv_rows& rows) {
 
 size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& rows, int x_dtype) {
     const int g = q_heads / v.heads;
-    const size_t streams = (size_t)2 * kCus * (D == 64 ? kStreamsPerCu<64> : kStreamsPerCu<128>) * kColumns * (D + 4) * sizeof(float);
+    const size_t streams = (size_t)2 * kStreams * kColumns * (D + 4) * sizeof(float);
     if (!may_have_prompts(x_dtype, g, rows)) return streams;
     return std::max(streams, (size_t)2 * kPrompts * kTile * (D + 4) * sizeof(float)) + tile_words_of(g, rows) * sizeof(int);
 }
@@ -1395,7 +1394,7 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     // what the chip holds at once is what the work is divided by; long lists of entries leave less LDS
     int per_cu = kStreamsPerCu<D>;
     while (per_cu > 1 && per_cu * (4 * kRing<D> * kv_block_bytes(D) + lds + 1024) > 160 * 1024) --per_cu;
-    const int streams = kCus * per_cu;
+    const int streams = 256 * per_cu;
     const auto streams_kernel = x_dtype == ESSA_F32 ? a.rows.row_start ? kv_attn_stream_kernel<D, true, true> : kv_attn_stream_kernel<D, true, false>
                                                     : a.rows.row_start ? kv_attn_stream_kernel<D, false, true> : kv_attn_stream_kernel<D, false, false>;
     streams_kernel<<<streams, 256, lds, st>>>(a);
