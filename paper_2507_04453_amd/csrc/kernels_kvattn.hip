@@ -1357,7 +1357,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
 
 namespace essa_k {
 
-constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;   // four a CU, one a CU
+// Four a CU, one a CU.  Heads of 128 launch three streams a CU; parts are reserved for four, which is what the prompt kernel's
+// are, so that a step recorded by itself leaves scratch that prompts fit into while it is alive.
+constexpr int kStreams = kKvAttnWorkgroups, kPrompts = 256;
+static_assert(kStreams * kColumns == kPrompts * kTile, "");
 
 static size_t tile_count(int g, const kv_rows& rows) { return (size_t)((long long)rows.R * g / kTile) + rows.n + 1; }
 static size_t tile_words_of(int g, const kv_rows& rows) { return (9 * tile_count(g, rows) + 8 + 3) / 4 * 4; }
