@@ -463,7 +463,8 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
  * Arithmetic: sums and softmax statistics in fp32.  bf16 Q: keys meet the queries on the bf16 MFMA with their codes exact,
  * weights and weights times scales are rounded to fp16 (with the largest weight at 2^13 or more and scales brought below 1, so that
  * values of any size from 1e-6 up keep its 11 bits); in calls of much work, entries with more than 64 pairs (row, query head) of a key head
- * have K, V and the weights rounded to fp16 instead.  fp32 Q: fp32 throughout.  Equal calls give equal bits.
+ * have K, V and the weights rounded to fp16 instead, so that a row's last bits depend on what else is in the call.  fp32 Q: fp32 throughout.
+ * Equal calls give equal bits.
  * The first call, and one larger than all before it, may allocate scratch (ESSA_ERR_STATE while a graph is recorded or alive). */
 #define ESSA_KV_ALL 0x1u
 essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,

@@ -59,6 +59,9 @@ __device__ __forceinline__ int wave_scan(int x, Op op) {
 // workgroups and all are short, a workgroup takes a whole one.
 // Lengths are counted in grains of 2^grain blocks: one block, unless the row could grow past an int.
 // ---------------------------------------------------------------------------------------------
+// kUnitCost: 256 sequences of 130 to 2100 tokens (28 heads on 4 of 128) take 49 us with 0, 42 with 3, 39.5 with 6 or 10, one of 2048 takes 12, 15, 13.5,
+// 14; every cut lies behind the cost, so kSnap is 3 more (14 instead of 9: one of 2048 14.4, 256 sequences 40.2).  kShort: 64
+// sequences of 512 take 15 us with 0, 11 with 40; 16 of 600 (16 heads of 64) 12.6 with 24, 9.4 with 40; one of 2048 13.5 with 40, 20.6 with 80.
 constexpr int kColumns = 64, kUnitCost = 6, kSnap = 9, kShort = 40;
 
 struct attn_args {
@@ -79,6 +82,8 @@ struct attn_args {
     int4* tile;                // [2 tiles] slot, len, row0, rows of the entry; which of its tiles, first stage, stages, length of a unit
     int tile_grain, tile_least;
 };
+// kTileCost and kTileSnap, in stages: 8192 rows take 714 us with a cost of 1, 584 with 3, 581 with 6; 16 prompts of 1024 rows 254, 237, 246; 32
+// times 300 rows behind 200 tokens 162 us with kTileSnap = 5, 116 with 8, 114 with 14 (16 of 1024: 251, 237, 216).
 constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
 // An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16), where a block
 // is unpacked once for 256 columns instead of once for 16 -- unless all of the call is little work for the stream kernel
@@ -340,7 +345,7 @@ __device__ __forceinline__ bool last_to_come(int* count, int others, int* last_o
 }
 
 // Parts w_first .. w_last of a unit, this workgroup's among them and written, become its result: in two steps, sixteen
-// consecutive ones and then the sixteens, so that a workgroup reads at most 16 + 48 of them.  A column's quads are neighbouring
+// consecutive ones and then the sixteens, so that a workgroup reads at most 16 + 64 of them.  A column's quads are neighbouring
 // lanes: all of them have read a part before one writes the sixteen's sum in its place.
 template <int D, int COLUMNS, int THREADS, class Finish>
 __device__ void join_parts(float* parts, int* done, int w_first, int w_last, int columns, int* last_one, Finish finish) {
@@ -421,6 +426,9 @@ __device__ __forceinline__ void load_raw(const kv_tensor& Q, long long at, uint3
 //   score = sum_group s <q, c - 8> + m sum q,      O = sum_group (p s) (c - 8) + sum p m.
 // bf16 queries: keys on the bf16 MFMA, every product exact; weights and weights times scales in fp16; sums in fp32.  fp32
 // queries: the same on the fp32 MFMA, with c - 8 as operands.
+// Why fp16: a weight's 11 bits are off by 2^-11 at most where the query it comes from was rounded to 2^-9 and its key and value to half of a
+// fifteenth of a range; outputs are 2e-4 to 6e-4 of their rms from 64 bits, those of bf16 1.7e-3 from their own rounding.  The fp32
+// MFMA, which would take weights as they are, has an eighth of the rate and operands that cost the vector ALU a conversion a code.
 // The running maximum moves only when a score passes it by kSlack (in the exponent of 2), which after the first blocks is rare:
 // weights stay below 2^(kLift + kSlack) = 2^15.
 // bf16 queries: the scales of values are anything from 2^-24 to 4370, and a weight times a scale has to fit into fp16 at either
@@ -755,9 +763,10 @@ __device__ __forceinline__ void put_out(const kv_tensor& Y, long long at, const 
 // A wave's blocks come through LDS, kRing of them on their way while one is worked on.  Workgroups a CU, each with 4 x kRing
 // blocks outstanding: four sequences of 100000 tokens (D = 128) take 98 us with two of them, 102 with three, 114 with four,
 // 256 sequences of 736 tokens 38, 35, 38.5; 64 sequences of 600 (D = 64) 25, 22, 16.
-// Long or many sequences are bound by memory: 4 x 100000 tokens of 8 heads 102 us (4.5 TB/s), 64 x 4096 60.5 us (5.0 TB/s).  A call
+// Long or many sequences are bound by memory: 4 x 100000 tokens of 8 heads 103 us (4.5 TB/s), 64 x 4096 62 us (4.9 TB/s).  A call
 // of little work is bound by what a workgroup does before its first block (list 4000 cycles, boundaries 4600, set-up 2000,
-// first loads 3600): 9.4 us for one sequence of 416 tokens.
+// first loads 3600): 9.4 us for one sequence of 416 tokens.  In between the vector ALU, unpacking, works half of the time (46 to 49 %), the matrix
+// cores 12 to 19 %, and waves wait for 24 to 37 % of theirs.
 template <int D> constexpr int kRing = 256 / D;
 template <int D> constexpr int kStreamsPerCu = D == 64 ? 4 : 3;
 template <int D, bool F32, bool OWN_ROWS>
@@ -920,14 +929,17 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 //
 // Scores^T = K Q^T and O^T = V^T P^T on the 32 x 32 x 16 MFMA.  Keys and values stand in LDS as fp16 numbers m + s q: rounded
 // once more (2^-11 of themselves) than in the stream kernel, because scales on the scores would be four multiply-adds for
-// each of them and the vector ALU is what this kernel is short of.  Rows of LDS are 16 bytes longer than their values: every
+// each of them, on a vector ALU that works as long as the matrix cores do.  Weights as there; a row's queries times the power of two that brings the
+// largest to 2^7 .. 2^8 are exact but for channels below 2^-24 of it.  Rows of LDS are 16 bytes longer than their values: every
 // 16 lanes that read together meet 64 different banks.  The tokens of a value's row stand in the order in which the first
 // product leaves the scores.
 // The two waves of a SIMD take turns, a barrier between them: while one has the matrix cores (the values of its last stage,
 // the scores of its next) the other has the vector ALU (the weights of its stage, its share of unpacking a stage to come).
 // Left to themselves both did the same at the same time, and the time was the sum of the two.
-// Bound by issue: a turn takes about 2000 cycles, of which the matrix cores work 1024.  A prompt of 8192 rows (28 heads on 4 of
-// 128) 554 us, 869 TFLOP/s; four times 512 rows behind 30000 tokens (40 on 8) 1289 us, 967 TFLOP/s.
+// A prompt of 8192 rows (28 heads on 4 of 128) 550 to 600 us, 800 to 880 TFLOP/s (by the card); four times 512 rows behind 30000
+// tokens (40 on 8) 1280 to 1350 us, 920 to 975 TFLOP/s.  Nothing is full: over the 8192 rows the matrix cores work 40 % of the time, the vector ALU
+// 38 %, LDS 31 % (78 % of what the products take: their operands, 4 KB in 32 cycles a CU, are all that it gives), and a turn is as
+// long as the longer of its two halves.
 // A NaN among the values must not reach columns that do not see it (0 times NaN): it is taken out and noted, and the
 // columns that see it are made NaN.
 // ---------------------------------------------------------------------------------------------
@@ -1377,8 +1389,9 @@ size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& r
 
 template <int D>
 static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
+    // one of 2048 tokens takes 11.2, 13.5, 18 us with 10, 16, 32, one of 65536 24.4, 22.1, 22.4, 256 of 256 20.7, 20.8, 24.3
     a.least = 16;
-    a.tile_least = 8;
+    a.tile_least = 8;          // (16 and 32: within 1 %)
     // the rows of units at their longest: every entry as long as the table allows
     const double units = ((double)a.rows.R * a.g / kColumns + a.rows.n) * a.v.heads, tiles = ((double)a.rows.R * a.g / kTile + a.rows.n) * a.v.heads;
     const double blocks = (double)((long long)a.v.max_pages << a.v.page_shift);

@@ -153,7 +153,7 @@ __global__ __launch_bounds__(kDeciders) void kv_extend_kernel(pages_view v, cons
 }
 
 // Freeing needs no decision: a workgroup an entry looks whether an earlier one names the same sequence, gives the pages back
-// and empties the table's row.  One launch, 2.8 us for two sequences and 5.0 for 86, where a fork's three took 9 and 16.
+// and empties the table's row.  One launch, 2.5 us for two sequences and 4.9 for 86, where a fork's three took 9 and 16.
 __global__ __launch_bounds__(256) void kv_free_kernel(pages_view v, const int32_t* seqs) {
     const int i = blockIdx.x, slot = seqs[i];
     if (slot < 0 || slot >= v.max_seqs) return;
