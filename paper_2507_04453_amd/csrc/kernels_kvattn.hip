@@ -445,7 +445,8 @@ __device__ __forceinline__ void load_raw(const kv_tensor& Q, long long at, uint3
 // end.  Below 1 a scale is what it is: the largest weight is between 2^13 and 2^15, so products stay below 2^15, and 2^-25, what a
 // product may lose to fp16's lower end, is 2^-38 of the largest weight with a scale of 1, 2^-20 of it with one of 2^-18 (values
 // near 1e-5).  Where a wave has seen a scale of 1 or more the group's are multiplied by the power of two that brings all below 1; it moves,
-// like the maximum, when a larger scale comes, and comes off in fp32 after the last block.
+// like the maximum, when a larger scale comes, and comes off in fp32 after the last block.  Looking for such scales takes a block 9
+// instructions: 2 to 6 rows of 48 sequences behind a window of 4096 63.1 -> 65.0 us, 256 single rows 36.4 -> 37.1; multiplying always, 66.6 and 38.9.
 // ---------------------------------------------------------------------------------------------
 constexpr float kSlack = 2.f;  // what a score may pass the running maximum by, as an exponent of 2
 constexpr float kTileSlack = 8.f, kTileLift = 4.f;            // prompts: weights alone have to fit into fp16
