@@ -321,6 +321,31 @@ essa_status essa_reward_finish(essa_ctx* ctx, const float* rowpart, int64_t n_bl
                                int K, float* F);
 
 /* ---------------------------------------------------------------------------------------------
+ * Log probabilities of tokens  (what a reward of Algorithm 1's "compute reward F" step is made of where answers are scored by the
+ * model's own probabilities, and what sampling and checking drafted tokens look at)
+ *
+ * For every row i of logits, z = scale * logits[i, :]:
+ *   logp[i, j]      z[tokens[i, j]] - log sum exp z; a negative token is padding and gives 0, one past V NaN
+ *   entropy[i]      - sum p log p in nats, p = softmax z
+ *   top_ids[i, r], top_logp[i, r]  the n_top largest logits in descending order, the lower token of equal ones first, and their log
+ *                   probabilities; -1 and -inf past the last token whose logit is not -inf
+ * A logit of -inf is a token that cannot come.  A row of nothing else gives logp -inf, entropy 0 and no top tokens; one that holds a
+ * NaN or a +inf gives NaN, and -1 for top_ids.  Sums are fp32.  Equal calls give equal bits.
+ *   logits   DEVICE [R] rows of V values of x_dtype at stride * i (in values), anywhere that a value may lie
+ *   scale    > 0 (1 / temperature); its product with log2(e) is finite
+ *   tokens   DEVICE int32 [R, n_tokens]   logp DEVICE float [R, n_tokens]   (n_tokens = 0: neither is looked at)
+ *   entropy  DEVICE float [R] or NULL
+ *   top_ids  DEVICE int32 [R, n_top]   top_logp DEVICE float [R, n_top]   (n_top = 0: neither is looked at)
+ * The first call, and one larger than all before it, may allocate (ESSA_ERR_STATE while a graph is recorded, for scratch also while one
+ * is alive).  essa_reward_accumulate with logp as Y, d_out = 1 and v = { 1 } gives every candidate the mean of its rows.
+ * ------------------------------------------------------------------------------------------- */
+#define ESSA_LOGPROB_MAX_TOKENS 4096
+#define ESSA_LOGPROB_MAX_TOP 64
+#define ESSA_LOGPROB_MAX_TOP_VOCAB (1 << 19)
+essa_status essa_token_logprobs(essa_ctx* ctx, const void* logits, int64_t stride, int x_dtype, int R, int V, float scale, const int32_t* tokens,
+                                int n_tokens, float* logp, float* entropy, int n_top, int32_t* top_ids, float* top_logp);
+
+/* ---------------------------------------------------------------------------------------------
  * Hot path 5: rank-weighted update  (paper: Algorithm 1, "each worker reconstructs the same
  * population and performs one CMA-ES update of (m, sigma, C)"; a reward is the 32-bit scalar workers
  * exchange)

@@ -4,7 +4,7 @@
 #include <cstring>
 #include <memory>
 
-#include "essa_internal.h"
+#include "logprob_internal.h"
 
 static thread_local std::string g_err;
 
@@ -59,6 +59,7 @@ extern "C" void essa_destroy(essa_ctx* ctx) {
     if (ctx->ws) (void)hipFree(ctx->ws);
     if (ctx->told_at) (void)hipHostFree(ctx->told_at);
     if (ctx->told) (void)hipEventDestroy(ctx->told);
+    if (ctx->counts) (void)hipFree(ctx->counts);
     for (hipEvent_t e : ctx->ev) (void)hipEventDestroy(e);
     delete ctx;
 }
@@ -1008,6 +1009,50 @@ extern "C" essa_status essa_reward_accumulate_group(essa_ctx* ctx, int n_items, 
 extern "C" essa_status essa_reward_accumulate(essa_ctx* ctx, const void* Y, int y_dtype, int R, int d_out, const float* v,
                                               const int32_t* row2cand, int K, float* F) {
     return essa_reward_accumulate_group(ctx, 1, &Y, &d_out, &v, y_dtype, R, row2cand, K, F);
+}
+
+extern "C" essa_status essa_token_logprobs(essa_ctx* ctx, const void* logits, int64_t stride, int x_dtype, int R, int V, float scale, const int32_t* tokens,
+                                           int n_tokens, float* logp, float* entropy, int n_top, int32_t* top_ids, float* top_logp) {
+    const char* who = "essa_token_logprobs";
+    if (!ctx) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (x_dtype != ESSA_F32 && x_dtype != ESSA_BF16) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: x_dtype %d", who, x_dtype);
+    if (R < 0 || R > (1 << 24) || V < 1 || V > (1 << 28)) return essa_fail(ESSA_ERR_SHAPE, "%s: R=%d not in [0, 2^24] or V=%d not in [1, 2^28]", who, R, V);
+    if (stride < V || stride > ((int64_t)1 << 32)) return essa_fail(ESSA_ERR_SHAPE, "%s: rows of %d logits, %lld apart", who, V, (long long)stride);
+    if (n_tokens < 0 || n_tokens > ESSA_LOGPROB_MAX_TOKENS || n_top < 0 || n_top > ESSA_LOGPROB_MAX_TOP)
+        return essa_fail(ESSA_ERR_SHAPE, "%s: n_tokens=%d not in [0, %d] or n_top=%d not in [0, %d]", who, n_tokens, ESSA_LOGPROB_MAX_TOKENS, n_top, ESSA_LOGPROB_MAX_TOP);
+    if (n_top > 0 && V > ESSA_LOGPROB_MAX_TOP_VOCAB)
+        return essa_fail(ESSA_ERR_UNSUPPORTED, "%s: the most probable of V=%d tokens, built for %d at most", who, V, ESSA_LOGPROB_MAX_TOP_VOCAB);
+    const float k = scale * 1.44269504088896340736f;
+    if (!(scale > 0.0f) || !(k - k == 0.0f)) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: scale=%g, it has to be above 0 and its product with log2(e) finite", who, (double)scale);
+    if (R == 0) return ESSA_OK;
+    if (!logits || (n_tokens > 0 && (!tokens || !logp)) || (n_top > 0 && (!top_ids || !top_logp))) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if ((uintptr_t)logits % (x_dtype == ESSA_F32 ? 4 : 2)) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: logits are not aligned to their values", who);
+    ESSA_HIP(hipSetDevice(ctx->device));
+    if (R < essa_k::kLogprobSplitRows && !ctx->counts) {
+        if (ctx->capturing) return essa_fail(ESSA_ERR_STATE, "%s: its first call makes its counts: run it once before essa_graph_begin", who);
+        void* p = nullptr;
+        const size_t bytes = essa_k::kLogprobSplitRows * sizeof(int32_t);
+        const hipError_t e = device_alloc(&p, bytes);
+        if (e != hipSuccess) return essa_fail(ESSA_ERR_OOM, "%s: hipMalloc of %zu bytes: %s", who, bytes, hipGetErrorString(e));
+        ctx->counts = (int32_t*)p;
+        ESSA_HIP(hipMemsetAsync(p, 0, bytes, ctx->stream));
+    }
+    ESSA_TRY(essa_ws_reserve(ctx, essa_k::token_logprobs_bytes(R, V, x_dtype, n_top)));
+    essa_k::logprob_args a{};
+    a.logits = logits;
+    a.stride = stride;
+    a.V = V;
+    a.n_tokens = n_tokens;
+    a.n_top = n_top;
+    a.scale = scale;
+    a.k = k;
+    a.tokens = tokens;
+    a.logp = logp;
+    a.entropy = entropy;
+    a.top_ids = top_ids;
+    a.top_logp = top_logp;
+    ESSA_HIP(essa_k::token_logprobs(ctx->stream, a, x_dtype, R, ctx->counts, ctx->ws));
+    return ESSA_OK;
 }
 
 // ---------------------------------------------------------------------------------------------

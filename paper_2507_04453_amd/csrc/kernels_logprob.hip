@@ -1,0 +1,432 @@
+// Log probabilities of given tokens, a row's entropy, and its most probable tokens, from one pass over the logits.
+//
+// With k = scale log2(e) and any number `down` (about -k max x), the weights 2^d, d = k x + down, give
+//   s = sum 2^d,  t = sum d 2^d:    log2 p_j = d_j - log2 s,    entropy / ln 2 = log2 s - t / s,
+// whatever `down` was rounded to, as long as all of a row use the same; sums of another `down` become this one's by
+// f = 2^(change), s f and f (t + change s).  Every lane keeps its own, and moves it when a value passes its weights' 2^kSlack.
+#include <algorithm>
+
+#include "forward_device.h"
+#include "logprob_internal.h"
+
+namespace {
+
+using essa_k::kLogprobSegment;
+using essa_k::logprob_args;
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kVec = 8;                        // values of a lane's load (two loads in fp32)
+constexpr int kLoad = 64 * kVec;               // values of a wave's
+constexpr float kSlack = 8.f;
+// What `down` is where a lane has seen nothing that counts.  Rows whose largest k x is beyond +-kHuge have sums of their own (see finish_row).
+constexpr float kHuge = 1e37f;
+constexpr int kCandidates = 512;
+
+__device__ __forceinline__ uint32_t ordered(float x) {         // as x is; -0 is 0
+    const int b = __float_as_int(x + 0.f);
+    return (uint32_t)(b ^ (b >> 31 | (int)0x80000000u));
+}
+
+struct row_sums {
+    float max, down, s, t;
+};
+__device__ __forceinline__ float down_of(float max, float k) {
+    const float z = max * k;
+    return z > kHuge ? -kHuge : z >= -kHuge ? -z : kHuge;      // nothing seen (-inf): kHuge
+}
+__device__ __forceinline__ void move_to(row_sums& a, float down) {
+    const float change = down - a.down, f = __builtin_amdgcn_exp2f(change);
+    a.t = f * (a.t + fmaxf(change, -2.f * kHuge) * a.s);
+    a.s *= f;
+    a.down = down;
+}
+
+// A row in memory: loads are of whole 16 bytes, so a row that begins inside of them begins `skip` values into its first load.
+template <bool F32>
+struct row_view {
+    const unsigned char* at;   // on 16 bytes
+    int skip, n;               // n: values up to the row's end, those in front of it included
+    __device__ __forceinline__ row_view(const logprob_args& a, int row) {
+        constexpr int SIZE = F32 ? 4 : 2;
+        const uint64_t p = (uint64_t)a.logits + (uint64_t)row * (uint64_t)a.stride * SIZE;
+        skip = (int)(p & 15) / SIZE;
+        at = (const unsigned char*)(p & ~(uint64_t)15);
+        n = a.V + skip;
+    }
+    __device__ __forceinline__ float value(int i) const { return F32 ? ((const float*)at)[i] : bf16_bits_to_f32(((const uint16_t*)at)[i]); }
+};
+template <bool F32>
+struct raw_values {
+    u32x4 w[F32 ? 2 : 1];
+};
+// a lane's eight values of load j: 8 lane .. + 7 of its kLoad (fp32: 4 lane .. + 3 of either half)
+template <bool F32>
+__device__ __forceinline__ int first_of(int j, int lane, int half) { return F32 ? j * kLoad + half * (kLoad / 2) + 4 * lane : j * kLoad + 8 * lane; }
+template <bool F32>
+__device__ __forceinline__ void load_values(const row_view<F32>& v, int j, int lane, raw_values<F32>& r) {
+    constexpr int PER = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
+    const int last = (v.n - 1) & ~(PER - 1);                   // the last load of 16 bytes that has a value of the row
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) r.w[i] = *(const u32x4*)(v.at + (size_t)min(first_of<F32>(j, lane, i), last) * SIZE);
+}
+template <bool F32>
+__device__ __forceinline__ void unpack(const row_view<F32>& v, int j, int lane, const raw_values<F32>& r, float (&x)[kVec]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) {
+            x[i] = __uint_as_float(r.w[0][i]);
+            x[4 + i] = __uint_as_float(r.w[1][i]);
+        } else {
+            x[2 * i] = __uint_as_float(r.w[0][i] << 16);
+            x[2 * i + 1] = __uint_as_float(r.w[0][i] & 0xffff0000u);
+        }
+    }
+    if (j == 0 || (j + 1) * kLoad > v.n) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const int at = F32 ? first_of<F32>(j, lane, i / 4) + i % 4 : first_of<F32>(j, lane, 0) + i;
+            x[i] = at >= v.skip && at < v.n ? x[i] : -INFINITY;
+        }
+    }
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x = fmaxf(x, __shfl_xor(x, m));
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
+    return x;
+}
+// all threads' sums as one, everywhere; waves: LDS
+__device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
+    const int wave = threadIdx.x / 64;
+    const float max = wave_max(a.max);
+    if ((threadIdx.x & 63) == 0) waves[0][wave] = max;
+    __syncthreads();
+    a.max = waves[0][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) a.max = fmaxf(a.max, waves[0][w]);
+    move_to(a, down_of(a.max, k));
+    const float s = wave_sum(a.s), t = wave_sum(a.t);
+    if ((threadIdx.x & 63) == 0) {
+        waves[1][wave] = s;
+        waves[2][wave] = t;
+    }
+    __syncthreads();
+    a.s = a.t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        a.s += waves[1][w];
+        a.t += waves[2][w];
+    }
+    __syncthreads();
+}
+
+// The n_top largest of a row.  A segment is kLogprobSegment consecutive values; with segments ordered by their largest value, the earlier
+// of equal ones first, the n_top largest values lie in the n_top first segments: a value outside of them has one in each in front of it.
+// seg: their largest values, in LDS.  put(rank, index, value): the result's places, all of them.
+struct top_lds {
+    int counts[2][3][kWaves];
+    int list[essa_k::kLogprobMostTop];
+    unsigned long long keys[kCandidates];
+    int found;
+    unsigned long long best[kWaves];
+};
+template <bool F32, class Put>
+__device__ void find_top(const row_view<F32>& v, const float* seg, int segments, int n_top, top_lds& l, Put put) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, want = min(n_top, segments);
+    // the want-th largest of the segments' keys, bit by bit (bf16: the lower half of a key says nothing about its order)
+    uint32_t limit = 0;
+    for (int bit = 31; bit >= (F32 ? 0 : 16); --bit) {
+        const uint32_t tried = limit | 1u << bit;
+        int count = 0;
+        for (int i = threadIdx.x; i < (segments + 63) / 64 * 64; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= tried));
+        if (lane == 0) l.counts[bit & 1][0][wave] = count;
+        __syncthreads();
+        count = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) count += l.counts[bit & 1][0][w];
+        if (count >= want) limit = tried;
+        if (count == want) break;
+    }
+    __syncthreads();
+    // segments at or above it, in order; of those whose upper bits are the limit's only as many as are wanted
+    int above = 0, equal = 0;
+    const uint32_t next = limit + (F32 ? 1u : 0x10000u);
+    {
+        int count = 0;
+        for (int i = threadIdx.x; i < (segments + 63) / 64 * 64; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= next));
+        if (lane == 0) l.counts[0][2][wave] = count;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) above += l.counts[0][2][w];
+    }
+    int at_above = 0;
+    for (int base = 0, turn = 0; base < segments; base += kThreads, turn ^= 1) {
+        const int i = base + (int)threadIdx.x;
+        const uint32_t key = i < segments ? ordered(seg[i]) : 0u;
+        const bool gt = i < segments && key >= next, eq = i < segments && key >= limit && key < next;
+        const unsigned long long g = __ballot(gt), e = __ballot(eq);
+        if (lane == 0) {
+            l.counts[turn][0][wave] = __popcll(g);
+            l.counts[turn][1][wave] = __popcll(e);
+        }
+        __syncthreads();
+        const unsigned long long below = (1ull << lane) - 1;
+        int my_above = at_above + __popcll(g & below), my_equal = equal + __popcll(e & below);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) {
+                my_above += l.counts[turn][0][w];
+                my_equal += l.counts[turn][1][w];
+            }
+            at_above += l.counts[turn][0][w];
+            equal += l.counts[turn][1][w];
+        }
+        if (gt) l.list[my_above] = i;
+        if (eq && above + my_equal < want) l.list[above + my_equal] = i;
+    }
+    if (threadIdx.x == 0) l.found = 0;
+    __syncthreads();
+    // their values that are not below the limit
+    const auto key_of = [&](int i) -> unsigned long long {     // of value i of the chosen segments; 0: none
+        const int at = l.list[i / kLogprobSegment] * kLogprobSegment + i % kLogprobSegment;
+        if (at < v.skip || at >= v.n) return 0;
+        const float x = v.value(at);
+        const uint32_t key = ordered(x);
+        return x > -INFINITY && key >= limit ? (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)(at - v.skip)) : 0;
+    };
+    const auto value_of = [](unsigned long long key) {
+        const uint32_t b = (uint32_t)(key >> 32);
+        return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+    };
+    for (int i = threadIdx.x; i < want * kLogprobSegment; i += kThreads) {     // whole waves: a segment is a multiple of 64
+        const unsigned long long key = key_of(i), has = __ballot(key != 0);
+        int first = 0;
+        if (lane == 0 && has) first = atomicAdd(&l.found, __popcll(has));
+        first = __shfl(first, 0) + __popcll(has & ((1ull << lane) - 1));
+        if (key && first < kCandidates) l.keys[first] = key;
+    }
+    __syncthreads();
+    const int found = l.found;
+    if (found <= kCandidates) {
+        for (int i = threadIdx.x; i < found; i += kThreads) {
+            const unsigned long long key = l.keys[i];
+            int rank = 0;
+            for (int o = 0; o < found; ++o) rank += l.keys[o] > key;
+            if (rank < n_top) put(rank, (int)(0xffffffffu - (uint32_t)key), value_of(key));
+        }
+        for (int i = found + threadIdx.x; i < n_top; i += kThreads) put(i, -1, -INFINITY);
+        return;
+    }
+    // more than that many, as where most values are alike: one after another
+    unsigned long long last = ~0ull;
+    for (int rank = 0; rank < n_top; ++rank) {
+        unsigned long long best = 0;
+        for (int i = threadIdx.x; i < want * kLogprobSegment; i += kThreads) {
+            const unsigned long long key = key_of(i);
+            if (key < last && key > best) best = key;
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const unsigned long long o = __shfl_xor(best, m);
+            best = o > best ? o : best;
+        }
+        if (lane == 0) l.best[wave] = best;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) best = l.best[w] > best ? l.best[w] : best;
+        __syncthreads();
+        if (threadIdx.x == 0) put(rank, best ? (int)(0xffffffffu - (uint32_t)best) : -1, best ? value_of(best) : -INFINITY);
+        last = best;
+    }
+}
+
+// What a row gives, once its sums are whole.  A row of huge numbers (all of its values the type's lowest, say) is summed again here,
+// as 2^(k (x - max)).
+template <bool F32, bool TOP>
+__device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, const float* seg, int segments, float (&waves)[3][kWaves], top_lds* l) {
+    const bool huge = fabsf(r.max) <= 3.402823466e38f && !(fabsf(r.max * a.k) <= kHuge);
+    if (huge) {
+        row_sums mine{r.max, 0.f, 0.f, 0.f};
+        for (int i = v.skip + (int)threadIdx.x; i < v.n; i += kThreads) {
+            const float d = (v.value(i) - r.max) * a.k, e = __builtin_amdgcn_exp2f(d);
+            mine.s += e;
+            mine.t = fmaf(e, fmaxf(d, -256.f), mine.t);
+        }
+        const float s = wave_sum(mine.s), t = wave_sum(mine.t);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) {
+            waves[1][threadIdx.x / 64] = s;
+            waves[2][threadIdx.x / 64] = t;
+        }
+        __syncthreads();
+        r.s = r.t = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            r.s += waves[1][w];
+            r.t += waves[2][w];
+        }
+    }
+    const bool nothing = r.max == -INFINITY && r.s == 0.f, bad = !(r.s == r.s) || r.max == INFINITY;
+    constexpr float kLn2 = 0.693147180559945309f;
+    const float log_s = __builtin_amdgcn_logf(r.s);
+    // from the largest value on, whose weight is 2^(k max + down): about 1.  Any logit that fp32 holds has a log probability then, if fp32 holds that.
+    const float most = ((huge ? 0.f : fmaf(r.max, a.k, r.down)) - log_s) * kLn2;
+    const auto logp = [&](float x) {
+        if (bad) return __uint_as_float(0x7fc00000u);
+        if (nothing || x == -INFINITY) return -INFINITY;
+        return fmaf(x - r.max, a.scale, most);
+    };
+    for (int i = threadIdx.x; i < a.n_tokens; i += kThreads) {
+        const size_t at = (size_t)row * a.n_tokens + i;
+        const int token = a.tokens[at];
+        a.logp[at] = token < 0 ? 0.f : token < a.V ? logp(v.value(v.skip + token)) : __uint_as_float(0x7fc00000u);
+    }
+    if (a.entropy && threadIdx.x == 0) a.entropy[row] = bad ? __uint_as_float(0x7fc00000u) : nothing ? 0.f : (log_s - r.t / r.s) * kLn2;
+    if constexpr (TOP) {
+        int32_t* ids = a.top_ids + (size_t)row * a.n_top;
+        float* lps = a.top_logp + (size_t)row * a.n_top;
+        if (nothing || bad) {
+            for (int i = threadIdx.x; i < a.n_top; i += kThreads) {
+                ids[i] = -1;
+                lps[i] = logp(-INFINITY);
+            }
+            return;
+        }
+        find_top<F32>(v, seg, segments, a.n_top, *l, [&](int rank, int index, float x) {
+            ids[rank] = index;
+            lps[rank] = logp(x);
+        });
+    }
+}
+
+template <bool F32, bool TOP>
+__global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a) {
+    extern __shared__ float seg[];                             // [segments of this part], then of the row
+    __shared__ float waves[3][kWaves];
+    __shared__ top_lds top;
+    __shared__ int last_one;
+    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const row_view<F32> v(a, row);
+    const int loads = (v.n + kLoad - 1) / kLoad, per = loads / a.parts, more = loads % a.parts;
+    const int j0 = part * per + min(part, more), j1 = j0 + per + (part < more);
+    constexpr int PER = kLoad / kLogprobSegment;               // segments of a load
+
+    row_sums r{-INFINITY, kHuge, 0.f, 0.f};
+    const auto take = [&](int j, const raw_values<F32>& raw) {
+        float x[kVec];
+        unpack<F32>(v, j, lane, raw, x);
+        float most = x[0], half = x[4];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            most = fmaxf(most, x[i]);
+            half = fmaxf(half, x[4 + i]);
+        }
+        if constexpr (TOP) {                                   // a segment is eight lanes' (fp32: sixteen lanes' of a half)
+            float p = F32 ? most : fmaxf(most, half), q = half;
+#pragma unroll
+            for (int m = 1; m < (F32 ? 16 : 8); m *= 2) {
+                p = fmaxf(p, __shfl_xor(p, m));
+                if (F32) q = fmaxf(q, __shfl_xor(q, m));
+            }
+            if (F32) {
+                if ((lane & 15) == 0) {
+                    seg[(j - j0) * PER + (lane >> 4)] = p;
+                    seg[(j - j0) * PER + 4 + (lane >> 4)] = q;
+                }
+            } else if ((lane & 7) == 0) seg[(j - j0) * PER + (lane >> 3)] = p;
+        }
+        most = fmaxf(most, half);
+        r.max = fmaxf(r.max, most);
+        if (__any(fmaf(most, a.k, r.down) > kSlack)) {
+            if (fmaf(most, a.k, r.down) > kSlack) move_to(r, -(most * a.k));
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float d = fmaf(x[i], a.k, r.down), e = __builtin_amdgcn_exp2f(d);
+            r.s += e;
+            r.t = fmaf(e, fmaxf(d, -256.f), r.t);              // where e is 0 d may be -inf
+        }
+    };
+    raw_values<F32> raw[4];
+    int j = j0 + wave;
+    for (; j + 3 * kWaves < j1; j += 4 * kWaves) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_values<F32>(v, j + i * kWaves, lane, raw[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) take(j + i * kWaves, raw[i]);
+    }
+    for (; j < j1; j += kWaves) {
+        load_values<F32>(v, j, lane, raw[0]);
+        take(j, raw[0]);
+    }
+    join_threads(r, a.k, waves);                               // its barriers are between the segments' writes and their reads
+    const int segments = loads * PER;
+    if (a.parts > 1) {
+        float* mine = a.sums + (size_t)blockIdx.x * 4;
+        if (threadIdx.x == 0) {
+            __hip_atomic_store(mine, r.max, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + 1, r.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + 2, r.t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        float* row_seg = a.segments + (size_t)row * a.row_segments;
+        if constexpr (TOP)
+            for (int i = threadIdx.x; i < (j1 - j0) * PER; i += kThreads) __hip_atomic_store(row_seg + j0 * PER + i, seg[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // written through; once all waves' stores have been acknowledged the count may say so, and the last part finishes the row
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const bool last = __hip_atomic_fetch_add(a.done + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.parts - 1;
+            if (last) __hip_atomic_store(a.done + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last_one = last;
+        }
+        __syncthreads();
+        if (!last_one) return;
+        if constexpr (TOP)
+            for (int i = threadIdx.x; i < segments; i += kThreads) seg[i] = __hip_atomic_load(row_seg + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        r = row_sums{-INFINITY, kHuge, 0.f, 0.f};
+        if ((int)threadIdx.x < a.parts) {
+            const float* p = a.sums + ((size_t)row * a.parts + threadIdx.x) * 4;
+            r.max = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            r.s = __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            r.t = __hip_atomic_load(p + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            r.down = down_of(r.max, a.k);
+        }
+        join_threads(r, a.k, waves);
+    }
+    finish_row<F32, TOP>(a, v, row, r, seg, segments, waves, &top);
+}
+
+}  // namespace
+
+namespace essa_k {
+
+static int loads_of(int V, int x_dtype) { return (V + (x_dtype == ESSA_F32 ? 3 : 7) + kLoad - 1) / kLoad; }
+// Parts of a row: enough workgroups for the chip, each with some loads a wave.
+static int parts_of(int R, int V, int x_dtype) {
+    const int loads = loads_of(V, x_dtype), most = std::min(kThreads, std::max(1, loads / (2 * kWaves)));
+    return R >= kLogprobSplitRows ? 1 : std::max(1, std::min(most, 1024 / R));
+}
+size_t token_logprobs_bytes(int R, int V, int x_dtype, int n_top) {
+    const int parts = parts_of(R, V, x_dtype);
+    return parts > 1 ? (size_t)R * (parts * 4 + (n_top ? loads_of(V, x_dtype) * (kLoad / kLogprobSegment) : 0)) * sizeof(float) : 0;
+}
+
+hipError_t token_logprobs(hipStream_t st, logprob_args a, int x_dtype, int R, int32_t* done, void* ws) {
+    a.parts = parts_of(R, a.V, x_dtype);
+    a.row_segments = loads_of(a.V, x_dtype) * (kLoad / kLogprobSegment);
+    a.done = done;
+    a.sums = (float*)ws;
+    a.segments = a.sums + (size_t)R * a.parts * 4;
+    const size_t lds = a.n_top ? (size_t)a.row_segments * sizeof(float) : 0;
+    const auto kernel = x_dtype == ESSA_F32 ? a.n_top ? token_logprobs_kernel<true, true> : token_logprobs_kernel<true, false>
+                                            : a.n_top ? token_logprobs_kernel<false, true> : token_logprobs_kernel<false, false>;
+    kernel<<<R * a.parts, kThreads, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace essa_k

@@ -18,7 +18,7 @@ __all__ = [
     "essa_cma_create_opt", "OPT_CMA", "OPT_ACTIVE_CMA", "OPT_SEP_CMA", "OPT_ES", "OPT_ARS",
     "VALIDATE", "essa_svdlora_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
     "KvCache", "KvBatch", "essa_kv_create", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact", "essa_kv_append", "essa_kv_read",
-    "essa_kv_attention", "KV_GROUP", "KV_BLOCK", "KV_SKIPPED", "KV_NO_PAGES", "KV_TOO_LONG", "KV_BAD_ENTRY", "KV_ALL",
+    "essa_kv_attention", "essa_token_logprobs", "LOGPROB_MAX_TOKENS", "LOGPROB_MAX_TOP", "LOGPROB_MAX_TOP_VOCAB", "KV_GROUP", "KV_BLOCK", "KV_SKIPPED", "KV_NO_PAGES", "KV_TOO_LONG", "KV_BAD_ENTRY", "KV_ALL",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libessa.so")
@@ -29,6 +29,7 @@ COMPUTE_W8A8, LORA_ONLY, BASE_ONLY, COMPUTE_BF16, VALIDATE = 1, 2, 4, 8, 16
 NOALLOC_SCRATCH_BYTES = 8 << 20
 MAX_GROUP = 8
 REWARD_BLOCK = 128
+LOGPROB_MAX_TOKENS, LOGPROB_MAX_TOP, LOGPROB_MAX_TOP_VOCAB = 4096, 64, 1 << 19
 KV_GROUP, KV_BLOCK = 64, 32
 KV_SKIPPED, KV_NO_PAGES, KV_TOO_LONG, KV_BAD_ENTRY = -1, -2, -3, -4
 KV_ALL = 1
@@ -46,7 +47,7 @@ EXPORTED_SYMBOLS = [
     "essa_graph_begin", "essa_graph_end", "essa_graph_launch", "essa_graph_destroy", "essa_cma_refresh_basis",
     "essa_cma_create_opt", "essa_cma_kind", "essa_svdlora_forward_noalloc",
     "essa_kv_pool_bytes", "essa_kv_create", "essa_kv_destroy", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact",
-    "essa_kv_append", "essa_kv_read", "essa_kv_attention",
+    "essa_kv_append", "essa_kv_read", "essa_kv_attention", "essa_token_logprobs",
 ]
 
 
@@ -123,6 +124,7 @@ def _load():
         "essa_reward_accumulate_group": (i32, [vp, i32, C.POINTER(vp), C.POINTER(i32), C.POINTER(vp), i32, i32, vp, i32, vp]),
         "essa_cmaes_update": (i32, [vp, vp, vp, vp, i32, vp]),
         "essa_rank_rewards": (i32, [vp, vp, i32, vp]),
+        "essa_token_logprobs": (i32, [vp, vp, i64, i32, i32, i32, f32, vp, i32, vp, vp, i32, vp, vp]),
         "essa_kv_pool_bytes": (C.c_size_t, [C.POINTER(_KvDesc)]),
         "essa_kv_create": (i32, [vp, C.POINTER(_KvDesc), C.POINTER(vp)]),
         "essa_kv_destroy": (None, [vp]),
@@ -556,6 +558,33 @@ def essa_reward_accumulate_group(ctx: Context, Ys, vs, row2cand: torch.Tensor, F
         yp[g], vp_[g], dd[g] = _dev(Y, None, "Y").value, _dev(v, torch.float32, "v").value, Y.shape[1]
     _check(lib.essa_reward_accumulate_group(ctx._h, n, yp, dd, vp_, yd, R, _dev(row2cand, torch.int32, "row2cand"), F.numel(),
                                             _dev(F, torch.float32, "F")))
+
+
+def essa_token_logprobs(ctx: Context, logits: torch.Tensor, tokens: torch.Tensor | None = None, logp: torch.Tensor | None = None, scale: float = 1.0,
+                        entropy: torch.Tensor | None = None, top_ids: torch.Tensor | None = None, top_logp: torch.Tensor | None = None):
+    """logits [R, V] (dense rows at any distance); tokens int32 [R] or [R, n], logp float32 of the same shape; entropy float32 [R];
+    top_ids int32 and top_logp float32 [R, n_top].  What is None is not computed."""
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1 and logits.numel() > 0):
+        raise ValueError("logits must be [R, V] with dense rows")
+    if not logits.is_cuda:
+        raise TypeError("logits must be a torch tensor on the GPU")
+    R, V = logits.shape
+    n_tokens = n_top = 0
+    if (tokens is None) != (logp is None) or (top_ids is None) != (top_logp is None):
+        raise ValueError("tokens and logp, top_ids and top_logp come together")
+    if tokens is not None:
+        n_tokens = 1 if tokens.dim() == 1 else tokens.shape[-1]
+        if tokens.dim() not in (1, 2) or tokens.shape[0] != R or logp.shape != tokens.shape:
+            raise ValueError("tokens must be [R] or [R, n], logp of the same shape")
+    if top_ids is not None:
+        n_top = top_ids.shape[-1]
+        if top_ids.dim() != 2 or top_ids.shape[0] != R or top_logp.shape != top_ids.shape:
+            raise ValueError("top_ids and top_logp must be [R, n_top]")
+    if entropy is not None and tuple(entropy.shape) != (R,):
+        raise ValueError("entropy must be [R]")
+    _check(lib.essa_token_logprobs(ctx._h, C.c_void_p(logits.data_ptr()), logits.stride(0) if R > 1 else V, _xdtype(logits), R, V, scale,
+                                   _dev(tokens, torch.int32, "tokens"), n_tokens, _dev(logp, torch.float32, "logp"), _dev(entropy, torch.float32, "entropy"), n_top,
+                                   _dev(top_ids, torch.int32, "top_ids"), _dev(top_logp, torch.float32, "top_logp")))
 
 
 def essa_cmaes_update(ctx: Context, cma: CmaState, seeds: torch.Tensor, rewards: torch.Tensor, order_out: torch.Tensor | None = None):
