@@ -463,6 +463,13 @@ essa_status essa_kv_extend(essa_ctx* ctx, essa_kv* kv, const int32_t* seqs, cons
 essa_status essa_kv_fork(essa_ctx* ctx, essa_kv* kv, const int32_t* src, const int32_t* dst, const int32_t* len, int n, int32_t* served);
 /* Frees sequences: essa_kv_fork with every src negative. */
 essa_status essa_kv_free(essa_ctx* ctx, essa_kv* kv, const int32_t* seqs, int n);
+/* Keeps some of a step's rows and takes the others back (drafted tokens that turned out right, in all layers).  Entry b's c rows of the batch are the last c
+ * tokens of its sequence; the rows path[row_start[b] + 0 .. keep[b] - 1] of them (numbers among the entry's rows, ascending) become the tokens behind the
+ * first len - c ones, the length becomes len - c + keep[b], and pages past it go back.  Their 4-bit values are moved as they are.
+ * Not served (ESSA_KV_BAD_ENTRY, the sequence is as it was): a sequence past max_seqs or named twice (from the second on), keep[b] not in [0, c], more rows
+ * than the sequence has tokens, a path that does not ascend or leaves the entry's rows, a page of these rows that another sequence holds too.
+ *   path DEVICE int32 [R]    keep DEVICE int32 [n]    served DEVICE int32 [n] or NULL: seqs[b], or why not */
+essa_status essa_kv_accept(essa_ctx* ctx, essa_kv* kv, const essa_kv_batch* batch, const int32_t* path, const int32_t* keep, int32_t* served);
 /* Moves the pages in use into pages 0 .. used - 1: those at or above `used` go, in ascending order, to the free ones
  * below it; table and refs follow.
  *   map_out  DEVICE int32 [n_pages] or NULL: a page's new index, -1 for a free one    used_out DEVICE int32 [1] or NULL */
@@ -494,6 +501,26 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
 #define ESSA_KV_ALL 0x1u
 essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
                               const essa_kv_batch* batch, float scale, int window, uint32_t flags, void* Y, int64_t y_stride, int y_dtype);
+
+/* The same with other sights.
+ *   sinks  with window > 0 the first `sinks` tokens of a sequence stay visible: the row at position p sees the tokens t <= p with
+ *          t > p - window or t < sinks.  Only the blocks of either are read.  (window = 0: everything up to p, whatever sinks is.)
+ *   tree   an entry's c rows are a tree of drafted tokens (several answers' next tokens checked in one call) instead of a run of them: row j sees every token in
+ *          front of them (t < len - c), and of the rows' own tokens that of row u where bit u % 64 of tree[row * tree_words + u / 64] is set
+ *          (its ancestors and itself, in a tree; what is not set it does not see, itself included, and rows past 64 tree_words nobody sees).  Bits from
+ *          c on are not looked at.  With a window the row's position p is len - c and one more for every other row that it sees, and the tokens in front of the
+ *          rows are seen if t > p - window or t < sinks; what is set among the rows is seen at any distance.
+ * tree: DEVICE uint64 [R, tree_words], 8-byte aligned, read by the call; tree_words = 0: no tree.  With neither sinks nor a tree the call gives the bits of
+ * essa_kv_attention. */
+#define ESSA_KV_TREE_WORDS 16
+typedef struct essa_kv_mask {
+    int32_t window;            /* 0: none                    */
+    int32_t sinks;
+    const uint64_t* tree;      /* DEVICE                     */
+    int32_t tree_words;        /* 0 .. ESSA_KV_TREE_WORDS    */
+} essa_kv_mask;
+essa_status essa_kv_attention_masked(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
+                                     const essa_kv_batch* batch, float scale, const essa_kv_mask* mask, void* Y, int64_t y_stride, int y_dtype);
 
 #ifdef __cplusplus
 }

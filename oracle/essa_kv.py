@@ -58,6 +58,38 @@ def kv_attention(q, k, v, rows, scale, window=0, causal=True):
     return y, mass, reach
 
 
+def kv_mask(L, rows, window=0, sinks=0, tree=None):
+    """[rows, L] truth values: which tokens the last `rows` rows of a sequence of L tokens see.  tree: [rows, rows] truth values, row j sees row u."""
+    base = L - rows
+    seen = np.zeros((rows, L), bool)
+    for j in range(rows):
+        if tree is None:
+            pos, end = base + j, base + j + 1
+        else:
+            mine = [u for u in range(rows) if tree[j][u] and base + u >= 0]
+            pos, end = base + len([u for u in mine if u != j]), base
+            seen[j, [base + u for u in mine]] = True
+        for t in range(max(0, end)):
+            if window == 0 or t > pos - window or t < sinks:
+                seen[j, t] = True
+    return seen
+
+
+def kv_attention_masked(q, k, v, seen, scale):
+    """As kv_attention, row j seeing the tokens seen[j]."""
+    rows, hq, D = q.shape
+    g = hq // k.shape[1]
+    y, mass, reach = np.zeros(q.shape), np.zeros(q.shape), np.zeros(q.shape[:2])
+    for j in range(rows):
+        at = np.flatnonzero(seen[j])
+        if not len(at):
+            continue
+        for h in range(hq):
+            one = kv_attention(q[j:j + 1, h:h + 1], k[at, h // g:h // g + 1], v[at, h // g:h // g + 1], 1, scale, causal=False)
+            y[j, h], mass[j, h], reach[j, h] = one[0][0, 0], one[1][0, 0], one[2][0, 0]
+    return y, mass, reach
+
+
 class KvPages:
     """The bookkeeping, entry after entry.  `tokens[s]` is a list of anything (what the sequence's tokens are), so that contents can
     be followed through forks; pages are sets of indices only."""
@@ -142,6 +174,31 @@ class KvPages:
                 self.refs[p] -= 1
         for b, new, tokens, _, _ in todo:
             self.pages[b], self.tokens[b] = new, tokens
+        return served
+
+    def accept(self, seqs, rows, path, keep):
+        """rows[b]: how many the entry has; path[b]: list of row numbers, of which the first keep[b] stay."""
+        served, seen = [], set()
+        for s, c, p, k in zip(seqs, rows, path, keep):
+            if s < 0:
+                served.append(KV_SKIPPED)
+                continue
+            bad = s >= self.max_seqs or s in seen
+            seen.add(s)
+            if not bad:
+                base = len(self.tokens[s]) - c
+                p = list(p[:max(k, 0)])
+                bad = k < 0 or k > c or base < 0 or any(x < 0 or x >= c for x in p) or any(a >= b for a, b in zip(p, p[1:]))
+                bad = bad or (c > 0 and any(self.refs[x] != 1 for x in self.pages[s][base // self.page:]))
+            if bad:
+                served.append(KV_BAD_ENTRY)
+                continue
+            self.tokens[s] = self.tokens[s][:base] + [self.tokens[s][base + x] for x in p]
+            need = self._need(len(self.tokens[s]))
+            for x in self.pages[s][need:]:
+                self.refs[x] -= 1
+            self.pages[s] = self.pages[s][:need]
+            served.append(s)
         return served
 
     def compact(self):

@@ -81,6 +81,11 @@ struct attn_args {
     int* tile_at;              // [tiles + 1]
     int4* tile;                // [2 tiles] slot, len, row0, rows of the entry; which of its tiles, first stage, stages, length of a unit
     int tile_grain, tile_least;
+    // kernels of masks (MASK) alone
+    int sinks;                 // first tokens that stay visible; 0 without a window
+    int sink_blocks;           // blocks, of which a window's worth in front of it is skipped; 0: none
+    int line_words;            // tree: 32-bit words a row, 0: no tree
+    const uint32_t* lines;     // [R, line_words]
 };
 // kTileCost and kTileSnap, in stages: 8192 rows take 714 us with a cost of 1, 584 with 3, 581 with 6; 16 prompts of 1024 rows 254, 237, 246; 32
 // times 300 rows behind 200 tokens 162 us with kTileSnap = 5, 116 with 8, 114 with 14 (16 of 1024: 251, 237, 216).
@@ -94,13 +99,17 @@ constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
 // either may be ahead, by up to a third.
 constexpr int kLittle = 8192;
 
+// With sinks (MASK) the blocks that hold them come first and lo more are left out behind them: block i of an entry's is i, or lo + i from sink_blocks on.
+template <bool MASK>
+__device__ __forceinline__ int left_out(int lo, int sink_blocks) { return MASK ? max(lo - sink_blocks, 0) : lo; }
 struct entry_span {            // the blocks that an entry's rows see, and how many units of kColumns columns it has for each key head
     int lo, n, groups;
 };
+template <bool MASK>
 __device__ __forceinline__ entry_span span_of(const attn_args& a, int len, int rows) {
     entry_span s;
     const int lo = a.window > 0 ? max(len - rows - a.window + 1, 0) : 0;
-    s.lo = lo / kKvBlock;
+    s.lo = left_out<MASK>(lo / kKvBlock, a.sink_blocks);
     s.n = rows > 0 && len > 0 ? (len + kKvBlock - 1) / kKvBlock - s.lo : 0;
     s.groups = (int)(((unsigned)(rows * a.g) + kColumns - 1) / kColumns);      // R rows of q_heads are below 2^31
     return s;
@@ -126,7 +135,7 @@ inline size_t list_bytes(int n, bool rows) { return rows ? (size_t)n * 2 * sizeo
 // sequence of 401 tokens.
 // Rows that see nothing are one workgroup's up to so many of an entry, everybody's beyond: 16000 rows of 28 heads of 128 took one 4.2 ms.
 constexpr int kBlank = 64;
-template <bool F32, bool OWN_ROWS>
+template <bool F32, bool OWN_ROWS, bool MASK>
 __device__ attn_list make_list(const attn_args& a, void* lds) {                // 256 threads
     __shared__ int waves[5][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
@@ -135,7 +144,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
         int work = 0;
         for (int b = lo; b < hi; ++b) {
             const kv_entry e = kv_entry_of(a.v, a.rows, b);
-            const entry_span s = span_of(a, e.len, e.rows);
+            const entry_span s = span_of<MASK>(a, e.len, e.rows);
             if (s.n) work += (int)min((long long)s.groups * a.v.heads * (s.n + kUnitCost), (long long)kLittle + 1);
         }
         work = wave_scan(work, [](int x, int y) { return x + y; });
@@ -147,7 +156,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     int length = 0, units = 0, longest = 0, rows = 0;          // (16 entries a thread at most: their rows are an int)
     for (int b = lo; b < hi; ++b) {
         const kv_entry e = kv_entry_of(a.v, a.rows, b);
-        const entry_span s = span_of(a, e.len, e.rows);
+        const entry_span s = span_of<MASK>(a, e.len, e.rows);
         const bool here = s.n && !is_prompt(a, l, e.rows);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.who[b] = int2{e.slot, e.len};
@@ -205,7 +214,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     l.even = uniform(total_units <= (int)gridDim.x && longest <= kShort && a.grain == 0 ? longest : 0);
     for (int b = lo; b < hi; ++b) {
         const int4 e = l.entry(b);
-        const entry_span s = span_of(a, e.y, e.w);
+        const entry_span s = span_of<MASK>(a, e.y, e.w);
         const bool here = s.n && !is_prompt(a, l, e.w);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.at[b] = l.even ? units_at * l.even : length_at;
@@ -233,19 +242,25 @@ __device__ __forceinline__ int entry_at(const attn_list& l, int n, int at) {
 // key head.
 // ---------------------------------------------------------------------------------------------
 struct tile_span {
-    int lo, n, columns;        // first stage, stages, columns
+    int lo, n, columns;        // first stage (MASK: stages left out behind the sinks'), stages, columns
 };
+template <bool MASK>
 __device__ __forceinline__ tile_span tile_of(const attn_args& a, int len, int rows, int which) {
     tile_span t;
     const int c0 = which * kTile;
     t.columns = min(rows * a.g - c0, kTile);                   // R rows of q_heads are below 2^31
-    const int first = len - rows + c0 / a.g, last = len - rows + (c0 + t.columns - 1) / a.g;      // positions
+    int first = len - rows + c0 / a.g, last = len - rows + (c0 + t.columns - 1) / a.g;            // positions
+    if (MASK && a.line_words) {                                // of a tree: anything from the first one's on
+        first = len - rows;
+        last = len - 1;
+    }
     const int lo = a.window > 0 ? max(first - a.window + 1, 0) : 0, hi = a.all ? len : min(last + 1, len);
-    t.lo = lo / kStage;
+    t.lo = left_out<MASK>(lo / kStage, (a.sink_blocks + 1) / 2);
     t.n = max((hi + kStage - 1) / kStage - t.lo, 0);
     return t;
 }
 // One workgroup of the stream kernel lists them for the prompt kernel behind it.
+template <bool MASK>
 __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           // 256 threads
     __shared__ int waves[4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
@@ -267,7 +282,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
     };
     const auto tiles_of = [&](int b) {
         const int4 e = l.entry(b);
-        return is_prompt(a, l, e.w) && span_of(a, e.y, e.w).n ? (int)(((unsigned)(e.w * a.g) + kTile - 1) / kTile) : 0;
+        return is_prompt(a, l, e.w) && span_of<MASK>(a, e.y, e.w).n ? (int)(((unsigned)(e.w * a.g) + kTile - 1) / kTile) : 0;
     };
     int mine = 0, tiles;
     for (int b = lo; b < hi; ++b) mine += tiles_of(b);
@@ -292,7 +307,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
                 else end = mid;
             }
             const int4 e = l.entry(b);
-            const tile_span t = tile_of(a, e.y, e.w, i - first[b]);
+            const tile_span t = tile_of<MASK>(a, e.y, e.w, i - first[b]);
             size = ((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost;
             a.tile[2 * i] = e;
             a.tile[2 * i + 1] = int4{i - first[b], t.lo, t.n, size};
@@ -303,6 +318,56 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
     }
     if (threadIdx.x == 0) a.tile_at[tiles] = done;
 }
+
+// ---------------------------------------------------------------------------------------------
+// Masks: what a column sees, 32 tokens at a time.
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : ~0u >> (32 - min(n, 32)); }
+struct column_sight {
+    int lo, hi;                // the window
+    int end;                   // no token from here on; 0: the column does not exist
+    int tree;                  // token of bit 0 of the line
+    const uint32_t* line;
+    bool any;                  // it sees a token
+    // pos: of its row; j: the row's number of the entry's `rows`; row: of all rows
+    __device__ __forceinline__ column_sight(const attn_args& a, int len, int rows, int j, int row, bool real) {
+        const int base = len - rows;
+        int pos = base + j;
+        hi = min(pos + 1, len);
+        end = hi;
+        tree = base;
+        line = nullptr;
+        any = false;
+        if (a.line_words) {
+            line = a.lines + (size_t)row * a.line_words;
+            // the row's depth: the others of its entry that it sees
+            const int words = min(a.line_words, (rows + 31) / 32);
+            pos = base;
+            for (int w = 0; w < words; ++w) {
+                const uint32_t seen = line[w] & bits_below(rows - 32 * w) & ~bits_below(-base - 32 * w);
+                any |= seen != 0;
+                pos += __popc(j >> 5 == w ? seen & ~(1u << (j & 31)) : seen);
+            }
+            hi = base;
+            end = len;
+        }
+        lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
+        any |= lo < hi || min(a.sinks, hi) > 0;
+        if (!real) {
+            any = false;
+            end = 0;
+        }
+    }
+    __device__ __forceinline__ uint32_t seen(const attn_args& a, int t0) const {
+        uint32_t bits = bits_below(hi - t0) & (~bits_below(lo - t0) | bits_below(a.sinks - t0));
+        if (a.line_words && t0 + 32 > tree) {
+            const int u = t0 - tree, w = u >> 5;
+            const uint32_t x = w >= 0 && w < a.line_words ? line[w] : 0u, y = w + 1 < a.line_words ? line[w + 1] : 0u;
+            bits |= __builtin_amdgcn_alignbit(y, x, (unsigned)u & 31u);
+        }
+        return bits & bits_below(end - t0);
+    }
+};
 
 // Where a boundary at `at` goes, `off` into a unit of length `size`; and which parts the unit at `unit_at` then lies in.
 template <int SNAP>
@@ -500,7 +565,7 @@ __device__ __forceinline__ void codes_f32(uint32_t w, float (&c)[8]) {
 __device__ __forceinline__ float half_of(const u32x4& r, int e) { return (float)as_f16(r[e >> 1])[e & 1]; }
 
 // a wave's columns: their queries as operands, what they see, the softmax so far
-template <int D, bool F32>
+template <int D, bool F32, bool MASK>
 struct attn_state {
     static constexpr int NG = D / kKvGroup, KK = D / 32;
     bf16x8 q16[F32 ? 1 : KK];
@@ -519,7 +584,7 @@ struct attn_state {
 
     // w: the lane's channels 32 k + 8 (lane / 16) .. + 7 as they are in memory; pos: position of the column's row; real: the column exists
     static constexpr int RAW = F32 ? 8 : 4;                    // words of 8 channels
-    __device__ __forceinline__ void start(const attn_args& a, uint32_t (&w)[KK][RAW], int len, int pos, bool real) {
+    __device__ __forceinline__ void start(const attn_args& a, uint32_t (&w)[KK][RAW], int len, int pos, bool real, bool sees) {
         // a negative scale is the queries' sign
         const uint32_t sign = a.scale < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
         bool finite;
@@ -572,7 +637,7 @@ struct attn_state {
         vlo = real ? (a.window > 0 ? max(pos - a.window + 1, 0) : 0) : 0;
         top = -kFar;
         down = kLift;
-        sum = real && !finite && vlo < vhi ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
+        sum = real && !finite && (MASK ? sees : vlo < vhi) ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
             mid[gr] = 0.f;
@@ -607,9 +672,10 @@ struct attn_state {
         for (int i = 0; i < 4; ++i) vs[i] = __builtin_bit_cast(uint32_t, as_f16(vs[i]) * lift);
     }
 
-    // `block`: in LDS; t0: its first token; whole: every column of the wave sees all of it; read: called once all of it has been read
-    template <class Read>
-    __device__ __forceinline__ void step(const unsigned char* block, int t0, bool whole, int lane, Read read) {
+    // `block`: in LDS; t0: its first token; whole: every column of the wave sees all of it; read: called once all of it has been read;
+    // sight (MASK): the tokens of it that the column sees, a bit each
+    template <class Read, class Sight>
+    __device__ __forceinline__ void step(const unsigned char* block, int t0, bool whole, int lane, Read read, Sight sight) {
         const int h = lane >> 4;
         kv_regs<D> r;
         read_block<D>(r, block, block + essa_k::kv_key_scales_at(D), lane);
@@ -645,10 +711,11 @@ struct attn_state {
         read_block<D>(r, block + essa_k::kv_values_at(D), block + essa_k::kv_value_scales_at(D), lane);
         bool seen[8];
         if (!whole) {
+            const uint32_t bits = MASK ? sight() >> (4 * h) : 0u;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int t = t0 + 16 * (e >> 2) + 4 * h + (e & 3);
-                seen[e] = t >= vlo && t < vhi;
+                seen[e] = MASK ? (bits >> (16 * (e >> 2) + (e & 3)) & 1u) != 0 : t >= vlo && t < vhi;
                 s[e] = seen[e] ? s[e] : -kFar;
             }
         }
@@ -780,7 +847,7 @@ __device__ __forceinline__ void put_out(const kv_tensor& Y, long long at, const 
 // cores 12 to 19 %, and waves wait for 24 to 37 % of theirs.
 template <int D> constexpr int kRing = 256 / D;
 template <int D> constexpr int kStreamsPerCu = D == 64 ? 4 : 3;
-template <int D, bool F32, bool OWN_ROWS>
+template <int D, bool F32, bool OWN_ROWS, bool MASK>
 __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(attn_args a) {
     constexpr int KK = D / 32, QUADS = D / 4, S = kRing<D>, BLOCK = essa_k::kv_block_bytes(D);
     extern __shared__ int4 list_lds[];
@@ -790,8 +857,8 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
     row_of* merged = (row_of*)ring;                            // [4]: after a unit's last block
     static_assert(sizeof(row_of) * 4 <= sizeof ring, "");
     __shared__ int last_one;
-    const attn_list list = make_list<F32, OWN_ROWS>(a, list_lds);
-    if (OWN_ROWS && a.tiles && blockIdx.x == gridDim.x - 1) plan_tiles(a, list);
+    const attn_list list = make_list<F32, OWN_ROWS, MASK>(a, list_lds);
+    if (OWN_ROWS && a.tiles && blockIdx.x == gridDim.x - 1) plan_tiles<MASK>(a, list);
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 4;
     const int total = uniform(list.at[a.rows.n]), part = list.even ? list.even : max(divide(total, (int)gridDim.x) + 1, a.least);
     const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
@@ -805,7 +872,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         const int4 e = list.entry(b);
         place p;
         p.entry = int4{uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w)};
-        p.sp = span_of(a, p.entry.y, p.entry.w);
+        p.sp = span_of<MASK>(a, p.entry.y, p.entry.w);
         p.grains = ((p.sp.n - 1) >> a.grain) + 1;
         p.size = list.even ? list.even : p.grains + kUnitCost;
         const int in = uniform(at - list.at[b]);
@@ -844,14 +911,40 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
             all_lo = a.window > 0 ? max(pos1 - a.window + 1, 0) : 0;
             some_hi = a.all ? len : min(pos1 + 1, len);
             all_hi = a.all ? len : min(pos0 + 1, len);
+            if (MASK && a.line_words) {                        // rows of a tree are anywhere from its first position on
+                some_lo = a.window > 0 ? max(len - rows - a.window + 1, 0) : 0;
+                all_lo = a.window > 0 ? max(len - a.window, 0) : 0;
+                some_hi = len;
+                all_hi = len - rows;
+            }
         }
-        const int b1 = min(sp.lo + stop, (some_hi + kKvBlock - 1) / kKvBlock);
-        int k = max(sp.lo + first, some_lo / kKvBlock) + stripe;
+        // the wave's blocks are k .. b1 - 1, every stripes-th; MASK: the k-th of the part's, the first `front` of them the sinks'
+        int b1 = min(sp.lo + stop, (some_hi + kKvBlock - 1) / kKvBlock);
+        int k = max(sp.lo + first, some_lo / kKvBlock) + stripe, front = 0, behind = 0;
+        if constexpr (MASK) {
+            front = 16 * tile < columns ? max(min(stop, a.sink_blocks) - first, 0) : 0;
+            const int from = max(max(first, a.sink_blocks), some_lo / kKvBlock - sp.lo);
+            behind = from - front + sp.lo;
+            b1 = front + max(b1 - sp.lo - from, 0);
+            k = stripe;
+        }
+        const auto block_of = [&](int k) { return !MASK ? k : k < front ? first + k : k + behind; };
         const int* table = a.v.table + (size_t)slot * a.v.max_pages;
-        int held = k >> a.v.page_shift, pages;                 // 64 entries of the table, from page `held` on
+        int held = block_of(k) >> a.v.page_shift, pages;       // 64 entries of the table, from page `held` on
+        int next_held = 0, next_pages = 0;                     // MASK: and from the window's first one on
         pages = (int)min((unsigned)table[min(held + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
-        auto block_at = [&](int k) {
-            const int f = k >> a.v.page_shift;
+        if (MASK && front > 0) {
+            next_held = (front + behind) >> a.v.page_shift;
+            next_pages = (int)min((unsigned)table[min(next_held + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
+        }
+        bool in_front = MASK && front > 0;
+        auto block_at = [&](int i) {
+            const int k = block_of(i), f = k >> a.v.page_shift;
+            if (MASK && in_front && i >= front) {
+                held = next_held;
+                pages = next_pages;
+                in_front = false;
+            }
             if (f >= held + 64) {
                 held = f;
                 pages = (int)min((unsigned)table[min(f + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
@@ -861,7 +954,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         const int column = 16 * tile + (lane & 15);
         const bool real = column < columns;
         const int x = r0 + (real ? column : 0), j = over_g(x), r = x - j * a.g;
-        uint32_t q[KK][attn_state<D, F32>::RAW];
+        uint32_t q[KK][attn_state<D, F32, MASK>::RAW];
         {
             const long long from = (long long)(row0 + j0 + j) * a.Q.stride + (long long)(head * a.g + r) * D + 8 * h;
 #pragma unroll
@@ -869,21 +962,24 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         }
         // waited for here: loads into LDS that the compiler does not know of would be waited for with them
         asm volatile("" : "+v"(pages));
+        if (MASK) asm volatile("" : "+v"(next_pages));
+        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real);
 #pragma unroll
         for (int i = 0; i < KK; ++i)
 #pragma unroll
-            for (int c = 0; c < attn_state<D, F32>::RAW; ++c) asm volatile("" : "+v"(q[i][c]));
+            for (int c = 0; c < attn_state<D, F32, MASK>::RAW; ++c) asm volatile("" : "+v"(q[i][c]));
         lds_barrier();                                         // the last unit's numbers have been read
         const uint32_t my_ring = (uint32_t)(uintptr_t)(lds_byte*)ring + wave * S * BLOCK;
         for (int i = 0; i < S; ++i)
             if (k + i * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + i * stripes), lane);
-        attn_state<D, F32> st;
-        st.start(a, q, len, len - rows + j0 + j, real);
+        attn_state<D, F32, MASK> st;
+        st.start(a, q, len, len - rows + j0 + j, real, MASK && sight.any);
         for (int i = 0; k < b1; k += stripes) {
             if (k + (S - 1) * stripes < b1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kBlockLoads<D>) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            st.step(ring + (wave * S + i) * BLOCK, k * kKvBlock, k * kKvBlock >= all_lo && (k + 1) * kKvBlock <= all_hi, lane,
-                    [&] { if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane); });
+            const int t0 = block_of(k) * kKvBlock;
+            st.step(ring + (wave * S + i) * BLOCK, t0, (t0 >= all_lo || (MASK && t0 + kKvBlock <= a.sinks)) && t0 + kKvBlock <= all_hi, lane,
+                    [&] { if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane); }, [&] { return sight.seen(a, t0); });
             i = i + 1 == S ? 0 : i + 1;
         }
         // the four quarters of a column's tokens, then the waves that share columns
@@ -927,7 +1023,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
     }
     // rows that see nothing: no unit holds them
     const int width = a.g * a.v.heads * QUADS;
-    const auto sees_nothing = [&](int b) { return list.at[b] == list.at[b + 1] && span_of(a, list.entry(b).y, list.entry(b).w).n == 0; };
+    const auto sees_nothing = [&](int b) { return list.at[b] == list.at[b + 1] && span_of<MASK>(a, list.entry(b).y, list.entry(b).w).n == 0; };
     for (int b = blockIdx.x; b < a.rows.n; b += gridDim.x)
         if (sees_nothing(b)) {
             const int4 e = list.entry(b);
@@ -1002,7 +1098,7 @@ struct tile_words {
     u32x4 v_s, v_m;
 };
 
-template <int D>
+template <int D, bool MASK>
 __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_args a) {
     constexpr int N = D / 64, KK = D / 16, OT = D / 32, QUADS = D / 4, NG = D / kKvGroup, KROW = tile_lds<D>::KROW, VROW = tile_lds<D>::VROW;
     __shared__ tile_lds<D> buffer[3];
@@ -1058,7 +1154,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
         const int from = max(at - unit_at - kTileCost, 0), to = min(min(size, end - unit_at) - kTileCost, grains);
         at = unit_at + size;
         const bool begins = from == 0, complete = begins && to == grains;
-        const int first = tile_lo + (from << a.tile_grain), stop = tile_lo + min(to << a.tile_grain, tile_n);
+        // stages; MASK: of those that are not left out
+        const int first = (MASK ? 0 : tile_lo) + (from << a.tile_grain), stop = (MASK ? 0 : tile_lo) + min(to << a.tile_grain, tile_n);
+        const int sink_stages = (a.sink_blocks + 1) / 2;
+        const auto stage_of = [&](int i) { return MASK && i >= sink_stages ? i + tile_lo : i; };
         const int c0 = which * kTile, columns = min(rows * a.g - c0, kTile), j0 = divide(c0, a.g), r0 = c0 - j0 * a.g;
         // this wave's columns
         const int column = 32 * wave + l;
@@ -1070,13 +1169,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             const int pos0 = len - rows + j0 + over_g(r0 + 32 * wave), pos1 = len - rows + j0 + over_g(r0 + min(32 * wave + 31, columns - 1));
             all_lo = a.window > 0 ? max(pos1 - a.window + 1, 0) : 0;
             all_hi = a.all ? len : min(pos0 + 1, len);
+            if (MASK && a.line_words) {
+                all_lo = a.window > 0 ? max(len - a.window, 0) : 0;
+                all_hi = len - rows;
+            }
         }
+        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real);
+        const bool sees_any = MASK ? sight.any : vlo < vhi;
         // a thread's words of a stage (its block of the two; past the end the last one's again)
         const int* table = a.v.table + (size_t)max(slot, 0) * a.v.max_pages;
         const int last_block = max((len + kKvBlock - 1) / kKvBlock - 1, 0);
         int held = -64, pages = 0;
-        const auto fetch = [&](int stage, tile_words<D>& w) {
-            const int k = min(2 * stage + bk, last_block), f = k >> a.v.page_shift;
+        const auto fetch = [&](int i, tile_words<D>& w) {
+            const int k = min(2 * stage_of(i) + bk, last_block), f = k >> a.v.page_shift;
             if (f >= held + 64) {
                 held = f;
                 pages = (int)min((unsigned)table[min(f + lane, a.v.max_pages - 1)], (unsigned)a.v.n_pages - 1u);
@@ -1110,7 +1215,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
         };
         // what must not get into LDS: values behind the last token, whatever the page holds, and NaN
         const auto clean = [&](int stage, tile_words<D>& w) {
-            const int t0 = kStage * stage + 32 * bk;
+            const int t0 = kStage * stage_of(stage) + 32 * bk;
             if (t0 + 32 > len) {
                 int left = len - t0 - 4 * v_h;
                 asm volatile("" : "+v"(left));                 // rare paths keep nothing in registers for their sake
@@ -1214,7 +1319,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                     q[k][2 * i] = (_Float16)(__uint_as_float(y << 16) * f);
                     q[k][2 * i + 1] = (_Float16)(__uint_as_float(y & 0xffff0000u) * f);
                 }
-            sum = real && !finite && vlo < vhi ? NAN : 0.f;
+            sum = real && !finite && sees_any ? NAN : 0.f;
         }
         const float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
         float top = -kFar, down = kTileLift;
@@ -1257,10 +1362,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 if (threadIdx.x < 2 * NG + 1) nans[(stage + 2) & 3][threadIdx.x] = 0;
                 if (stage + 2 < stop) fetch(stage + 2, ahead);
                 {
-                    const int t0 = kStage * stage;
+                    const int t0 = kStage * stage_of(stage);
                     const unsigned any_nan = nans[stage & 3][2 * NG];
-                    const bool whole = t0 >= all_lo && t0 + kStage <= all_hi;
-                    if (!whole) {
+                    const bool whole = (t0 >= all_lo || (MASK && t0 + kStage <= a.sinks)) && t0 + kStage <= all_hi;
+                    if (MASK && !whole) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t bits = sight.seen(a, t0 + 32 * i) >> (4 * hh);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) s[i][k] = bits >> ((k & 3) + 8 * (k >> 2)) & 1u ? s[i][k] : -INFINITY;
+                        }
+                    } else if (!whole) {
                         int lo = vlo - t0 - 4 * hh, hi = vhi - t0 - 4 * hh;
                         asm volatile("" : "+v"(lo), "+v"(hi)); // or every token's bounds stand in registers all the time
 #pragma unroll
@@ -1301,7 +1413,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                         for (int gr = 0; gr < NG; ++gr) {
                             bool sees = false;
 #pragma unroll 1
-                            for (int t = 0; t < kStage; ++t) sees |= (nans[stage & 3][2 * gr + (t >> 5)] >> (t & 31) & 1) && t0 + t >= vlo && t0 + t < vhi;
+                            for (int t = 0; t < (MASK ? 0 : kStage); ++t) sees |= (nans[stage & 3][2 * gr + (t >> 5)] >> (t & 31) & 1) && t0 + t >= vlo && t0 + t < vhi;
+                            if (MASK) sees = (nans[stage & 3][2 * gr] & sight.seen(a, t0)) | (nans[stage & 3][2 * gr + 1] & sight.seen(a, t0 + 32));
                             if (sees)
 #pragma unroll
                                 for (int ot = 0; ot < 2; ++ot)
@@ -1409,7 +1522,7 @@ size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& r
     return std::max(streams, (size_t)2 * kPrompts * kTile * (D + 4) * sizeof(float)) + tile_words_of(g, rows) * sizeof(int);
 }
 
-template <int D>
+template <int D, bool MASK>
 static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     // one of 2048 tokens takes 11.2, 13.5, 18 us with 10, 16, 32, one of 65536 24.4, 22.1, 22.4, 256 of 256 20.7, 20.8, 24.3
     a.least = 16;
@@ -1433,15 +1546,15 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     int per_cu = kStreamsPerCu<D>;
     while (per_cu > 1 && per_cu * (4 * kRing<D> * kv_block_bytes(D) + lds + 1024) > 160 * 1024) --per_cu;
     const int streams = 256 * per_cu;
-    const auto streams_kernel = x_dtype == ESSA_F32 ? a.rows.row_start ? kv_attn_stream_kernel<D, true, true> : kv_attn_stream_kernel<D, true, false>
-                                                    : a.rows.row_start ? kv_attn_stream_kernel<D, false, true> : kv_attn_stream_kernel<D, false, false>;
+    const auto streams_kernel = x_dtype == ESSA_F32 ? a.rows.row_start ? kv_attn_stream_kernel<D, true, true, MASK> : kv_attn_stream_kernel<D, true, false, MASK>
+                                                    : a.rows.row_start ? kv_attn_stream_kernel<D, false, true, MASK> : kv_attn_stream_kernel<D, false, false, MASK>;
     streams_kernel<<<streams, 256, lds, st>>>(a);
-    if (prompts) kv_attn_prompt_kernel<D><<<kPrompts, kTileThreads, 0, st>>>(a);
+    if (prompts) kv_attn_prompt_kernel<D, MASK><<<kPrompts, kTileThreads, 0, st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale2,
-                        int window, bool all, int32_t* done, void* ws) {
+                        int window, bool all, int32_t* done, void* ws, const kv_mask& mask) {
     attn_args a{};
     a.v = v;
     a.Q = Q;
@@ -1453,7 +1566,13 @@ hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor
     a.window = window < v.max_len ? window : 0;               // what reaches past every token is none; so positions less a window stay ints
     a.all = all;
     a.done = done;
-    return D == 64 ? run<64>(st, a, ws, Q.dtype) : run<128>(st, a, ws, Q.dtype);
+    // without a window nothing is out of sight, and sinks say nothing
+    a.sinks = a.window ? std::min(mask.sinks, v.max_len) : 0;
+    a.sink_blocks = (a.sinks + kKvBlock - 1) / kKvBlock;
+    a.line_words = 2 * mask.tree_words;
+    a.lines = (const uint32_t*)mask.tree;
+    if (a.sinks || a.line_words) return D == 64 ? run<64, true>(st, a, ws, Q.dtype) : run<128, true>(st, a, ws, Q.dtype);
+    return D == 64 ? run<64, false>(st, a, ws, Q.dtype) : run<128, false>(st, a, ws, Q.dtype);
 }
 
 }  // namespace essa_k

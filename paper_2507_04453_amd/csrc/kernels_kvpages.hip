@@ -262,6 +262,140 @@ __global__ __launch_bounds__(256) void kv_fork_tables_kernel(pages_view v, const
     if (threadIdx.x == 0) v.len[b] = tokens;
 }
 
+// Keeping a path of a tree's rows.  Entry b's rows are its sequence's last ones; rows path[0] < path[1] < .. of them stay, row path[i] as token base + i,
+// so that a token only ever moves towards the front: with the blocks that tokens move into done in order, each read whole before it is written, no
+// token is overwritten before it has moved.  Workgroup (b, y) looks for itself whether the entry can be served and moves its share of the heads of
+// all layers; (b, 0) leaves the answer for the launch that gives pages back.
+struct accept_entry {
+    int ok;                    // the sequence, or why not
+    int row0, base, keep, moved;   // moved: the first row of the path that is not where it was
+};
+__device__ accept_entry accept_of(const pages_view& v, const essa_k::kv_rows& rows, const int32_t* path, const int32_t* keep, int b) {     // 256 threads
+    __shared__ int moved;
+    accept_entry e{rows.seqs[b], b, 0, keep[b], 0};
+    int c = 1;
+    if (rows.row_start) {
+        e.row0 = min(max(rows.row_start[b], 0), rows.R);
+        c = min(max(rows.row_start[b + 1], e.row0), rows.R) - e.row0;
+    }
+    if (e.ok < 0) {
+        e.ok = ESSA_KV_SKIPPED;
+        return e;
+    }
+    if (threadIdx.x == 0) moved = e.keep;
+    bool bad = e.ok >= v.max_seqs;
+    const int len = bad ? 0 : v.length(e.ok);
+    e.base = len - c;
+    bad |= e.keep < 0 || e.keep > c || e.base < 0;
+    for (int j = threadIdx.x; j < b; j += 256) bad |= rows.seqs[j] == e.ok;
+    __syncthreads();
+    if (!bad) {
+        int first = e.keep;
+        for (int i = threadIdx.x; i < e.keep; i += 256) {
+            const int p = path[e.row0 + i];
+            bad |= p < 0 || p >= c || (i > 0 && path[e.row0 + i - 1] >= p);
+            if (p != i) first = min(first, i);
+        }
+        if (first < e.keep) atomicMin(&moved, first);
+        // rows in a page that somebody else holds are not this sequence's to move
+        if (c > 0)
+            for (int f = e.base / v.page_tokens + (int)threadIdx.x; f < v.pages(len); f += 256) bad |= v.refs[v.page(e.ok, f)] != 1;
+    }
+    if (__syncthreads_or(bad)) e.ok = ESSA_KV_BAD_ENTRY;
+    e.moved = moved;
+    return e;
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void kv_accept_move_kernel(pages_view v, essa_k::kv_rows rows, const int32_t* path, const int32_t* keep, unsigned char* pool,
+                                                             long long page_bytes, int head_bytes, int heads) {
+    constexpr int NG = D / kKvGroup, KW = D / 64, VECS = D / 32;               // of a thread: words of keys, vectors of values
+    __shared__ unsigned char codes[kKvBlock][D + 4];
+    const int b = blockIdx.x;
+    const accept_entry e = accept_of(v, rows, path, keep, b);
+    if (blockIdx.y == 0 && threadIdx.x == 0) v.s.entry_ok[b] = e.ok;
+    if (e.ok < 0 || e.moved >= e.keep) return;
+    const int tok = threadIdx.x / 8, part = threadIdx.x % 8, per_page = v.page_tokens / kKvBlock;
+    const auto block_at = [&](int head, int block) {
+        return pool + v.page(e.ok, block / per_page) * page_bytes + (long long)head * head_bytes + (size_t)(block % per_page) * essa_k::kv_block_bytes(D);
+    };
+    const auto scale_at = [&](int side, int group, int t) { return (side ? essa_k::kv_value_scales_at(D) : essa_k::kv_key_scales_at(D)) + kv_scale_at(group, t); };
+    for (int head = blockIdx.y; head < heads; head += gridDim.y)
+        for (int block = (e.base + e.moved) / kKvBlock; block * kKvBlock < e.base + e.keep; ++block) {
+            const int t0 = block * kKvBlock, first = max(e.base + e.moved - t0, 0), last = min(e.base + e.keep - t0, kKvBlock);
+            unsigned char* out = block_at(head, block);
+            const bool mine = tok >= first && tok < last;
+            uint32_t words[KW];
+            uint16_t s = 0, m = 0;
+            __syncthreads();                                   // the codes of the block before have been read
+            if (mine) {
+                const int from = e.base + path[e.row0 + t0 + tok - e.base], ft = from % kKvBlock;
+                const unsigned char* in = block_at(head, from / kKvBlock);
+#pragma unroll
+                for (int w = 0; w < KW; ++w) words[w] = *(const uint32_t*)(in + kv_key_word<D>(ft, part * KW + w));
+                if (part < 2 * NG) {
+                    const uint16_t* p = (const uint16_t*)(in + scale_at(part / NG, part % NG, ft));
+                    s = p[0];
+                    m = p[8];
+                }
+                u32x4 x[VECS];
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) {
+                    const int q = part * VECS + i;
+                    x[i] = *(const u32x4*)(in + essa_k::kv_values_at(D) + 1024 * (q >> 4) + 16 * (kv_run(ft) * 16 + (q & 15)));
+                }
+#pragma unroll
+                for (int i = 0; i < VECS; ++i) {
+                    const int q = part * VECS + i;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) codes[tok][64 * (q >> 4) + 16 * k + (q & 15)] = x[i][k] >> kv_shift(kv_element(ft)) & 15;
+                }
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // everything that moves into this block has been read
+            __syncthreads();
+            if (mine) {
+#pragma unroll
+                for (int w = 0; w < KW; ++w) *(uint32_t*)(out + kv_key_word<D>(tok, part * KW + w)) = words[w];
+                if (part < 2 * NG) {
+                    uint16_t* p = (uint16_t*)(out + scale_at(part / NG, part % NG, tok));
+                    p[0] = s;
+                    p[8] = m;
+                }
+            }
+            for (int i = threadIdx.x; i < 4 * D; i += 256) {
+                const int h = i / D, c = i % D;
+                uint32_t w = 0, keep_bits = 0;
+#pragma unroll
+                for (int el = 0; el < 8; ++el) {
+                    const int t = (el & 3) + 16 * (el >> 2) + 4 * h;
+                    if (t < first || t >= last) keep_bits |= 15u << kv_shift(el);
+                    else w |= (uint32_t)codes[t][c] << kv_shift(el);
+                }
+                if (keep_bits == ~0u) continue;
+                uint32_t* to = (uint32_t*)(out + kv_value_word<D>(h, c));
+                *to = (*to & keep_bits) | w;
+            }
+        }
+}
+
+__global__ __launch_bounds__(256) void kv_accept_tables_kernel(pages_view v, essa_k::kv_rows rows, const int32_t* keep, int32_t* served) {
+    const int b = blockIdx.x, ok = v.s.entry_ok[b];
+    if (threadIdx.x == 0 && served) served[b] = ok;
+    if (ok < 0) return;
+    int c = 1;
+    if (rows.row_start) {
+        const int row0 = min(max(rows.row_start[b], 0), rows.R);
+        c = min(max(rows.row_start[b + 1], row0), rows.R) - row0;
+    }
+    const int len = v.length(ok), now = len - c + keep[b];
+    __syncthreads();                                           // everybody has the old length
+    for (int f = v.pages(now) + (int)threadIdx.x; f < v.pages(len); f += 256) {
+        atomicSub(&v.refs[v.page(ok, f)], 1);
+        v.table[(size_t)ok * v.max_pages + f] = -1;
+    }
+    if (threadIdx.x == 0) v.len[ok] = now;
+}
+
 // Compaction: count the pages in use, list those above and the holes below (ascending), and every page's new index.
 __global__ __launch_bounds__(kDeciders) void kv_compact_decide_kernel(pages_view v, int32_t* map_out, int32_t* used_out) {
     constexpr int PER = 8;
@@ -377,6 +511,16 @@ hipError_t kv_fork(hipStream_t st, const essa_kv* kv, const int32_t* src, const 
     kv_fork_decide_kernel<<<1, kDeciders, (d.max_seqs + (d.max_seqs + 31) / 32 + n + 1) * sizeof(int), st>>>(v, src, dst, len, n, served);
     kv_fork_copy_kernel<<<dim3(n, std::min(heads, 64)), 256, 0, st>>>(v, src, dst, (unsigned char*)d.pool, (long long)per_head * heads, per_head, block, heads);
     kv_fork_tables_kernel<<<n, 256, 0, st>>>(v, dst);
+    return hipGetLastError();
+}
+
+hipError_t kv_accept(hipStream_t st, const essa_kv* kv, const kv_rows& rows, const int32_t* path, const int32_t* keep, int32_t* served) {
+    const essa_kv_desc& d = kv->d;
+    const pages_view v = view_of(kv);
+    const int per_head = kv_block_bytes(d.head_dim) * (d.page_tokens / kKvBlock), heads = d.layers * d.n_kv_heads;
+    const auto move = d.head_dim == 64 ? kv_accept_move_kernel<64> : kv_accept_move_kernel<128>;
+    move<<<dim3(rows.n, std::min(heads, 64)), 256, 0, st>>>(v, rows, path, keep, (unsigned char*)d.pool, (long long)per_head * heads, per_head, heads);
+    kv_accept_tables_kernel<<<rows.n, 256, 0, st>>>(v, rows, keep, served);
     return hipGetLastError();
 }
 

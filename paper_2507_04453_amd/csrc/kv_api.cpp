@@ -146,6 +146,16 @@ static essa_k::kv_view view_of(const essa_kv* kv, int layer) {
 }
 static essa_k::kv_rows rows_of(const essa_kv_batch* b) { return {b->seqs, b->row_start, b->n, b->R}; }
 
+extern "C" essa_status essa_kv_accept(essa_ctx* ctx, essa_kv* kv, const essa_kv_batch* batch, const int32_t* path, const int32_t* keep, int32_t* served) {
+    ESSA_TRY(check_kv(ctx, kv, "essa_kv_accept"));
+    ESSA_TRY(check_rows(kv, 0, batch, "essa_kv_accept"));
+    if (batch->n == 0) return ESSA_OK;
+    if (!keep || (batch->R > 0 && !path)) return essa_fail(ESSA_ERR_INVALID_ARG, "essa_kv_accept: NULL argument");
+    ESSA_HIP(hipSetDevice(ctx->device));
+    ESSA_HIP(essa_k::kv_accept(ctx->stream, kv, rows_of(batch), path, keep, served));
+    return ESSA_OK;
+}
+
 extern "C" essa_status essa_kv_append(essa_ctx* ctx, essa_kv* kv, int layer, const void* K, int64_t k_stride, const void* V, int64_t v_stride, int x_dtype,
                                       const essa_kv_batch* batch) {
     ESSA_TRY(check_kv(ctx, kv, "essa_kv_append"));
@@ -174,9 +184,8 @@ extern "C" essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer,
     return ESSA_OK;
 }
 
-extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
-                                         const essa_kv_batch* batch, float scale, int window, uint32_t flags, void* Y, int64_t y_stride, int y_dtype) {
-    const char* who = "essa_kv_attention";
+static essa_status attention(const char* who, essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
+                             const essa_kv_batch* batch, float scale, int window, uint32_t flags, const essa_k::kv_mask& mask, void* Y, int64_t y_stride, int y_dtype) {
     ESSA_TRY(check_kv(ctx, kv, who));
     ESSA_TRY(check_rows(kv, layer, batch, who));
     if (n_q_heads < 1 || n_q_heads > 32768 || n_q_heads % kv->d.n_kv_heads)
@@ -197,6 +206,23 @@ extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int l
     const essa_k::kv_rows rows = rows_of(batch);
     ESSA_TRY(essa_ws_reserve(ctx, essa_k::kv_attention_bytes(v, kv->d.head_dim, n_q_heads, rows, x_dtype)));
     ESSA_HIP(essa_k::kv_attention(ctx->stream, v, kv->d.head_dim, q, y, n_q_heads, rows, scale2, window, (flags & ESSA_KV_ALL) != 0,
-                                  essa_k::kv_scratch_of(kv).done, ctx->ws));
+                                  essa_k::kv_scratch_of(kv).done, ctx->ws, mask));
     return ESSA_OK;
+}
+
+extern "C" essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
+                                         const essa_kv_batch* batch, float scale, int window, uint32_t flags, void* Y, int64_t y_stride, int y_dtype) {
+    return attention("essa_kv_attention", ctx, kv, layer, Q, q_stride, x_dtype, n_q_heads, batch, scale, window, flags, {}, Y, y_stride, y_dtype);
+}
+
+extern "C" essa_status essa_kv_attention_masked(essa_ctx* ctx, const essa_kv* kv, int layer, const void* Q, int64_t q_stride, int x_dtype, int n_q_heads,
+                                                const essa_kv_batch* batch, float scale, const essa_kv_mask* mask, void* Y, int64_t y_stride, int y_dtype) {
+    const char* who = "essa_kv_attention_masked";
+    if (!mask) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: NULL argument", who);
+    if (mask->sinks < 0) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: sinks=%d", who, mask->sinks);
+    if (mask->tree_words < 0 || mask->tree_words > ESSA_KV_TREE_WORDS)
+        return essa_fail(ESSA_ERR_SHAPE, "%s: tree_words=%d not in [0, %d]", who, mask->tree_words, ESSA_KV_TREE_WORDS);
+    if (mask->tree_words > 0 && batch && batch->R > 0 && !mask->tree) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: tree is NULL", who);
+    if (mask->tree_words > 0 && (uintptr_t)mask->tree % 8) return essa_fail(ESSA_ERR_INVALID_ARG, "%s: tree is not aligned to its words", who);
+    return attention(who, ctx, kv, layer, Q, q_stride, x_dtype, n_q_heads, batch, scale, mask->window, 0, {mask->sinks, mask->tree_words, mask->tree}, Y, y_stride, y_dtype);
 }

@@ -47,6 +47,12 @@ struct kv_tensor {             // R rows of heads * D values
     int aligned;               // rows begin on 16 bytes
 };
 
+struct kv_mask {
+    int sinks = 0;
+    int tree_words = 0;        // 64-bit words a row; 0: no tree
+    const uint64_t* tree = nullptr;
+};
+
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kKvAttnWorkgroups = 1024;    // four a CU
 
@@ -67,10 +73,12 @@ hipError_t kv_extend(hipStream_t st, const essa_kv* kv, const int32_t* seqs, con
 hipError_t kv_fork(hipStream_t st, const essa_kv* kv, const int32_t* src /*null: free*/, const int32_t* dst, const int32_t* len, int n, int32_t* served);
 hipError_t kv_compact(hipStream_t st, const essa_kv* kv, int32_t* map_out, int32_t* used_out);
 
+hipError_t kv_accept(hipStream_t st, const essa_kv* kv, const kv_rows& rows, const int32_t* path, const int32_t* keep, int32_t* served);
+
 hipError_t kv_append(hipStream_t st, const kv_view& v, int D, const kv_tensor& K, const kv_tensor& V, const kv_rows& rows);
 hipError_t kv_read(hipStream_t st, const kv_view& v, int D, const kv_tensor& K, const kv_tensor& V, const kv_rows& rows);
 
 size_t kv_attention_bytes(const kv_view& v, int D, int q_heads, const kv_rows& rows, int x_dtype);
 hipError_t kv_attention(hipStream_t st, const kv_view& v, int D, const kv_tensor& Q, const kv_tensor& Y, int q_heads, const kv_rows& rows, float scale2 /*times log2(e)*/,
-                        int window, bool all, int32_t* done, void* ws);
+                        int window, bool all, int32_t* done, void* ws, const kv_mask& mask);
 }  // namespace essa_k

@@ -18,7 +18,7 @@ __all__ = [
     "essa_cma_create_opt", "OPT_CMA", "OPT_ACTIVE_CMA", "OPT_SEP_CMA", "OPT_ES", "OPT_ARS",
     "VALIDATE", "essa_svdlora_forward_noalloc", "NOALLOC_SCRATCH_BYTES",
     "KvCache", "KvBatch", "essa_kv_create", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact", "essa_kv_append", "essa_kv_read",
-    "essa_kv_attention", "essa_token_logprobs", "LOGPROB_MAX_TOKENS", "LOGPROB_MAX_TOP", "LOGPROB_MAX_TOP_VOCAB", "KV_GROUP", "KV_BLOCK", "KV_SKIPPED", "KV_NO_PAGES", "KV_TOO_LONG", "KV_BAD_ENTRY", "KV_ALL",
+    "essa_kv_attention", "essa_kv_accept", "KV_TREE_WORDS", "essa_token_logprobs", "LOGPROB_MAX_TOKENS", "LOGPROB_MAX_TOP", "LOGPROB_MAX_TOP_VOCAB", "KV_GROUP", "KV_BLOCK", "KV_SKIPPED", "KV_NO_PAGES", "KV_TOO_LONG", "KV_BAD_ENTRY", "KV_ALL",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libessa.so")
@@ -33,6 +33,7 @@ LOGPROB_MAX_TOKENS, LOGPROB_MAX_TOP, LOGPROB_MAX_TOP_VOCAB = 4096, 64, 1 << 19
 KV_GROUP, KV_BLOCK = 64, 32
 KV_SKIPPED, KV_NO_PAGES, KV_TOO_LONG, KV_BAD_ENTRY = -1, -2, -3, -4
 KV_ALL = 1
+KV_TREE_WORDS = 16
 OPT_CMA, OPT_ACTIVE_CMA, OPT_SEP_CMA, OPT_ES, OPT_ARS = 0, 1, 2, 3, 4
 
 EXPORTED_SYMBOLS = [
@@ -47,7 +48,7 @@ EXPORTED_SYMBOLS = [
     "essa_graph_begin", "essa_graph_end", "essa_graph_launch", "essa_graph_destroy", "essa_cma_refresh_basis",
     "essa_cma_create_opt", "essa_cma_kind", "essa_svdlora_forward_noalloc",
     "essa_kv_pool_bytes", "essa_kv_create", "essa_kv_destroy", "essa_kv_extend", "essa_kv_fork", "essa_kv_free", "essa_kv_compact",
-    "essa_kv_append", "essa_kv_read", "essa_kv_attention", "essa_token_logprobs",
+    "essa_kv_append", "essa_kv_read", "essa_kv_attention", "essa_token_logprobs", "essa_kv_attention_masked", "essa_kv_accept",
 ]
 
 
@@ -76,6 +77,10 @@ class _FwdItem(C.Structure):
 class _KvDesc(C.Structure):
     _fields_ = [("layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int32),
                 ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("pool", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p), ("refs", C.c_void_p)]
+
+
+class _KvMask(C.Structure):
+    _fields_ = [("window", C.c_int32), ("sinks", C.c_int32), ("tree", C.c_void_p), ("tree_words", C.c_int32)]
 
 
 class _KvBatch(C.Structure):
@@ -134,6 +139,8 @@ def _load():
         "essa_kv_compact": (i32, [vp, vp, vp, vp]),
         "essa_kv_append": (i32, [vp, vp, i32, vp, i64, vp, i64, i32, C.POINTER(_KvBatch)]),
         "essa_kv_read": (i32, [vp, vp, i32, vp, i64, vp, i64, i32, C.POINTER(_KvBatch)]),
+        "essa_kv_accept": (i32, [vp, vp, C.POINTER(_KvBatch), vp, vp, vp]),
+        "essa_kv_attention_masked": (i32, [vp, vp, i32, vp, i64, i32, i32, C.POINTER(_KvBatch), f32, C.POINTER(_KvMask), vp, i64, i32]),
         "essa_kv_attention": (i32, [vp, vp, i32, vp, i64, i32, i32, C.POINTER(_KvBatch), f32, i32, u32, vp, i64, i32]),
     }
     for name, (res, args) in sig.items():
@@ -682,6 +689,13 @@ def essa_kv_free(ctx: Context, kv: KvCache, seqs: torch.Tensor):
     _check(lib.essa_kv_free(ctx._h, kv._h, _entries(kv, "seqs", seqs, n), n))
 
 
+def essa_kv_accept(ctx: Context, kv: KvCache, batch: KvBatch, path: torch.Tensor, keep: torch.Tensor, served: torch.Tensor | None = None):
+    """Of each entry's rows the first keep[b] that its part of path names (ascending) stay, in all layers; the others are taken back."""
+    if path.numel() != batch.R or keep.numel() != batch.n:
+        raise ValueError("path must hold one entry a row (%d), keep one a sequence (%d)" % (batch.R, batch.n))
+    _check(lib.essa_kv_accept(ctx._h, kv._h, batch.ref, _dev(path, torch.int32, "path"), _dev(keep, torch.int32, "keep"), _entries(kv, "served", served, batch.n)))
+
+
 def essa_kv_compact(ctx: Context, kv: KvCache, map_out: torch.Tensor | None = None, used_out: torch.Tensor | None = None):
     if (map_out is not None and map_out.numel() != kv.n_pages) or (used_out is not None and used_out.numel() != 1):
         raise ValueError("map_out must be [n_pages], used_out [1]")
@@ -719,9 +733,23 @@ def essa_kv_read(ctx: Context, kv: KvCache, layer: int, K: torch.Tensor, V: torc
 
 
 def essa_kv_attention(ctx: Context, kv: KvCache, layer: int, Q: torch.Tensor, Y: torch.Tensor, batch: KvBatch, scale: float, window: int = 0,
-                      causal: bool = True):
-    """Q, Y: [R, n_q_heads, head_dim] (or [R, n_q_heads * head_dim]); window 0: none."""
+                      causal: bool = True, sinks: int = 0, tree: torch.Tensor | None = None):
+    """Q, Y: [R, n_q_heads, head_dim] (or [R, n_q_heads * head_dim]); window 0: none.  sinks: first tokens that stay visible behind a window.
+    tree: int64 [R, words] (or [R]): an entry's rows are a tree, and bit u % 64 of a row's word u / 64 says that it sees row u of its entry."""
     heads = Q.shape[1] if Q.dim() == 3 else Q.shape[-1] // kv.head_dim
     q, qs = _kv_rows(Q, batch.R, heads, kv.head_dim, "Q")
     y, ys = _kv_rows(Y, batch.R, heads, kv.head_dim, "Y")
+    if sinks or tree is not None:
+        if not causal:
+            raise ValueError("sinks and trees are causal")
+        words = 0
+        if tree is not None:
+            if tree.dim() not in (1, 2) or tree.shape[0] != batch.R:
+                raise ValueError("tree must be [R, words] or [R]")
+            words = 1 if tree.dim() == 1 else tree.shape[1]
+            if words < 1:
+                raise ValueError("tree must have a word a row")
+        mask = _KvMask(window, sinks, _dev(tree, torch.int64, "tree"), words)
+        _check(lib.essa_kv_attention_masked(ctx._h, kv._h, layer, q, qs, _xdtype(Q), heads, batch.ref, scale, C.byref(mask), y, ys, _ydtype(Y)))
+        return
     _check(lib.essa_kv_attention(ctx._h, kv._h, layer, q, qs, _xdtype(Q), heads, batch.ref, scale, window, 0 if causal else KV_ALL, y, ys, _ydtype(Y)))
