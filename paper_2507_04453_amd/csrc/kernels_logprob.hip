@@ -20,7 +20,6 @@ constexpr int kLoad = 64 * kVec;               // values of a wave's
 constexpr float kSlack = 8.f;
 // What `down` is where a lane has seen nothing that counts.  Rows whose largest k x is beyond +-kHuge have sums of their own (see finish_row).
 constexpr float kHuge = 1e37f;
-constexpr int kCandidates = 512;
 
 __device__ __forceinline__ uint32_t ordered(float x) {         // as x is; -0 is 0
     const int b = __float_as_int(x + 0.f);
@@ -100,6 +99,17 @@ __device__ __forceinline__ float wave_sum(float x) {
     for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
     return x;
 }
+// over a lane's 8 or 16 neighbours, without a trip through LDS
+template <int N>
+__device__ __forceinline__ float neighbours_max(float x) {
+#define STEP(ctrl) x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl, 0xf, 0xf, true)))
+    STEP(0xb1);                                                // quad_perm 1 0 3 2
+    STEP(0x4e);                                                // quad_perm 2 3 0 1
+    STEP(0x141);                                               // row_half_mirror
+    if (N == 16) STEP(0x140);                                  // row_mirror
+#undef STEP
+    return x;
+}
 // all threads' sums as one, everywhere; waves: LDS
 __device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
     const int wave = threadIdx.x / 64;
@@ -125,90 +135,147 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
     __syncthreads();
 }
 
-// The n_top largest of a row.  A segment is kLogprobSegment consecutive values; with segments ordered by their largest value, the earlier
-// of equal ones first, the n_top largest values lie in the n_top first segments: a value outside of them has one in each in front of it.
-// seg: their largest values, in LDS.  put(rank, index, value): the result's places, all of them.
+// ---------------------------------------------------------------------------------------------
+// The n_top largest of a row.  A segment is kLogprobSegment consecutive values, of which `seg` (LDS) holds the largest.  With segments ordered by
+// it, the earlier of equal ones first, the n_top largest values lie in the n_top first segments: a value outside of them has one in each
+// in front of it.  So a few segments are read again, and of them what is not below a limit that n_top values reach is put in order.
+// The limit is the n_top-th largest of the threads' own segments' largest (upper half of the bits: a little less): 256 numbers instead of
+// thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
+// segments themselves are found, bit by bit; where too many values do, they are taken one after another.
+// ---------------------------------------------------------------------------------------------
+constexpr int kSegments = 256, kCandidates = 512;
 struct top_lds {
+    uint32_t best[kThreads];
     int counts[2][3][kWaves];
-    int list[essa_k::kLogprobMostTop];
+    int list[kSegments];
     unsigned long long keys[kCandidates];
-    int found;
-    unsigned long long best[kWaves];
+    int segments, found;
+    unsigned long long most[kWaves];
 };
-template <bool F32, class Put>
-__device__ void find_top(const row_view<F32>& v, const float* seg, int segments, int n_top, top_lds& l, Put put) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, want = min(n_top, segments);
-    // the want-th largest of the segments' keys, bit by bit (bf16: the lower half of a key says nothing about its order)
+// The largest number with at least `want` of a wave's keys (N a lane) at or above it and `bits` upper bits.
+template <int N>
+__device__ __forceinline__ uint32_t limit_of(const uint32_t (&key)[N], int want, int bits) {
     uint32_t limit = 0;
-    for (int bit = 31; bit >= (F32 ? 0 : 16); --bit) {
+    for (int bit = 31; bit >= 32 - bits; --bit) {
         const uint32_t tried = limit | 1u << bit;
         int count = 0;
-        for (int i = threadIdx.x; i < (segments + 63) / 64 * 64; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= tried));
-        if (lane == 0) l.counts[bit & 1][0][wave] = count;
+#pragma unroll
+        for (int i = 0; i < N; ++i) count += __popcll(__ballot(key[i] >= tried));
+        if (count >= want) {
+            limit = tried;
+            if (count == want) break;
+        }
+    }
+    return limit;
+}
+// The `want` first segments into l.list: returns the limit that parts them from the rest.
+template <bool F32>
+__device__ __attribute__((noinline)) uint32_t first_segments(const float* seg, int segments, int want, top_lds& l) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, whole = (segments + 63) & ~63;
+    const auto count_from = [&](uint32_t from, int slot) {
+        int count = 0;
+        for (int i = threadIdx.x; i < whole; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= from));
+        if (lane == 0) l.counts[slot & 1][0][wave] = count;
         __syncthreads();
         count = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) count += l.counts[bit & 1][0][w];
-        if (count >= want) limit = tried;
-        if (count == want) break;
-    }
-    __syncthreads();
-    // segments at or above it, in order; of those whose upper bits are the limit's only as many as are wanted
-    int above = 0, equal = 0;
+        for (int w = 0; w < kWaves; ++w) count += l.counts[slot & 1][0][w];
+        return count;
+    };
+    uint32_t limit = 0;                                        // (bf16: the lower half of a key says nothing about its order)
+    for (int bit = 31; bit >= (F32 ? 0 : 16); --bit)
+        if (count_from(limit | 1u << bit, bit) >= want) limit |= 1u << bit;
     const uint32_t next = limit + (F32 ? 1u : 0x10000u);
-    {
-        int count = 0;
-        for (int i = threadIdx.x; i < (segments + 63) / 64 * 64; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= next));
-        if (lane == 0) l.counts[0][2][wave] = count;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) above += l.counts[0][2][w];
-    }
-    int at_above = 0;
+    const int above = count_from(next, 1);
+    __syncthreads();
+    // those above it, and the first ones of those at it
+    int at_above = 0, equal = 0;
     for (int base = 0, turn = 0; base < segments; base += kThreads, turn ^= 1) {
         const int i = base + (int)threadIdx.x;
         const uint32_t key = i < segments ? ordered(seg[i]) : 0u;
         const bool gt = i < segments && key >= next, eq = i < segments && key >= limit && key < next;
-        const unsigned long long g = __ballot(gt), e = __ballot(eq);
+        const unsigned long long g = __ballot(gt), e = __ballot(eq), below = (1ull << lane) - 1;
         if (lane == 0) {
-            l.counts[turn][0][wave] = __popcll(g);
-            l.counts[turn][1][wave] = __popcll(e);
+            l.counts[turn][1][wave] = __popcll(g);
+            l.counts[turn][2][wave] = __popcll(e);
         }
         __syncthreads();
-        const unsigned long long below = (1ull << lane) - 1;
         int my_above = at_above + __popcll(g & below), my_equal = equal + __popcll(e & below);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             if (w < wave) {
-                my_above += l.counts[turn][0][w];
-                my_equal += l.counts[turn][1][w];
+                my_above += l.counts[turn][1][w];
+                my_equal += l.counts[turn][2][w];
             }
-            at_above += l.counts[turn][0][w];
-            equal += l.counts[turn][1][w];
+            at_above += l.counts[turn][1][w];
+            equal += l.counts[turn][2][w];
         }
         if (gt) l.list[my_above] = i;
         if (eq && above + my_equal < want) l.list[above + my_equal] = i;
     }
-    if (threadIdx.x == 0) l.found = 0;
     __syncthreads();
-    // their values that are not below the limit
-    const auto key_of = [&](int i) -> unsigned long long {     // of value i of the chosen segments; 0: none
-        const int at = l.list[i / kLogprobSegment] * kLogprobSegment + i % kLogprobSegment;
-        if (at < v.skip || at >= v.n) return 0;
-        const float x = v.value(at);
+    return limit;
+}
+// put(rank, index, value): the result's places, all of them.  wave-wide appends: at most one atomic a wave
+__device__ __forceinline__ int places(int* count, bool mine) {
+    const int lane = threadIdx.x & 63;
+    const unsigned long long has = __ballot(mine);
+    int first = 0;
+    if (lane == 0 && has) first = atomicAdd(count, __popcll(has));
+    return __builtin_amdgcn_readfirstlane(first) + __popcll(has & ((1ull << lane) - 1));
+}
+template <bool F32, class Put>
+__device__ void find_top(const row_view<F32>& v, const float* seg, int segments, int n_top, top_lds& l, Put put) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, want = min(n_top, segments);
+    {
+        float best = -INFINITY;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < segments; i += kThreads) best = fmaxf(best, seg[i]);
+        l.best[threadIdx.x] = (int)threadIdx.x < segments ? ordered(best) : 0u;
+        if (threadIdx.x == 0) l.segments = l.found = 0;
+    }
+    __syncthreads();
+    uint32_t mine[kThreads / 64];
+#pragma unroll
+    for (int i = 0; i < kThreads / 64; ++i) mine[i] = l.best[64 * i + lane];
+    uint32_t limit = limit_of(mine, want, 16);                 // (every wave finds the same)
+    const int whole = (segments + 63) & ~63;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < whole; i += kThreads) {
+        const bool in = i < segments && ordered(seg[min(i, segments - 1)]) >= limit;
+        if (__any(in)) {
+            const int at = places(&l.segments, in);
+            if (in && at < kSegments) l.list[at] = i;
+        }
+    }
+    __syncthreads();
+    int chosen = l.segments;
+    if (chosen > kSegments) {
+        limit = first_segments<F32>(seg, segments, want, l);
+        chosen = want;
+    }
+    const auto key_of = [&](int at, float x) -> unsigned long long {           // of value `at` of the row; 0: none
         const uint32_t key = ordered(x);
-        return x > -INFINITY && key >= limit ? (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)(at - v.skip)) : 0;
+        return at >= v.skip && at < v.n && x > -INFINITY && key >= limit ? (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)(at - v.skip)) : 0;
     };
     const auto value_of = [](unsigned long long key) {
         const uint32_t b = (uint32_t)(key >> 32);
         return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
     };
-    for (int i = threadIdx.x; i < want * kLogprobSegment; i += kThreads) {     // whole waves: a segment is a multiple of 64
-        const unsigned long long key = key_of(i), has = __ballot(key != 0);
-        int first = 0;
-        if (lane == 0 && has) first = atomicAdd(&l.found, __popcll(has));
-        first = __shfl(first, 0) + __popcll(has & ((1ull << lane) - 1));
-        if (key && first < kCandidates) l.keys[first] = key;
+    constexpr int PER = F32 ? 4 : 8, LOADS = kLogprobSegment / PER;            // of 16 bytes
+    for (int i = threadIdx.x; i < ((chosen * LOADS + 63) & ~63); i += kThreads) {
+        const bool real = i < chosen * LOADS;
+        const int first = l.list[real ? i / LOADS : 0] * kLogprobSegment + i % LOADS * PER;
+        const u32x4 w = *(const u32x4*)(v.at + (size_t)min(first, (v.n - 1) & ~(PER - 1)) * (F32 ? 4 : 2));
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const float x = __uint_as_float(F32 ? w[k & 3] : k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+            const unsigned long long key = real ? key_of(first + k, x) : 0;
+            if (__any(key != 0)) {
+                const int at = places(&l.found, key != 0);
+                if (key && at < kCandidates) l.keys[at] = key;
+            }
+        }
     }
     __syncthreads();
     const int found = l.found;
@@ -216,18 +283,19 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
         for (int i = threadIdx.x; i < found; i += kThreads) {
             const unsigned long long key = l.keys[i];
             int rank = 0;
+#pragma unroll 8
             for (int o = 0; o < found; ++o) rank += l.keys[o] > key;
             if (rank < n_top) put(rank, (int)(0xffffffffu - (uint32_t)key), value_of(key));
         }
         for (int i = found + threadIdx.x; i < n_top; i += kThreads) put(i, -1, -INFINITY);
         return;
     }
-    // more than that many, as where most values are alike: one after another
     unsigned long long last = ~0ull;
     for (int rank = 0; rank < n_top; ++rank) {
         unsigned long long best = 0;
-        for (int i = threadIdx.x; i < want * kLogprobSegment; i += kThreads) {
-            const unsigned long long key = key_of(i);
+        for (int i = threadIdx.x; i < chosen * kLogprobSegment; i += kThreads) {
+            const int at = l.list[i / kLogprobSegment] * kLogprobSegment + i % kLogprobSegment;
+            const unsigned long long key = key_of(at, v.value(min(at, v.n - 1)));
             if (key < last && key > best) best = key;
         }
 #pragma unroll
@@ -235,10 +303,10 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
             const unsigned long long o = __shfl_xor(best, m);
             best = o > best ? o : best;
         }
-        if (lane == 0) l.best[wave] = best;
+        if (lane == 0) l.most[wave] = best;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) best = l.best[w] > best ? l.best[w] : best;
+        for (int w = 0; w < kWaves; ++w) best = l.most[w] > best ? l.most[w] : best;
         __syncthreads();
         if (threadIdx.x == 0) put(rank, best ? (int)(0xffffffffu - (uint32_t)best) : -1, best ? value_of(best) : -INFINITY);
         last = best;
@@ -328,11 +396,8 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
         }
         if constexpr (TOP) {                                   // a segment is eight lanes' (fp32: sixteen lanes' of a half)
             float p = F32 ? most : fmaxf(most, half), q = half;
-#pragma unroll
-            for (int m = 1; m < (F32 ? 16 : 8); m *= 2) {
-                p = fmaxf(p, __shfl_xor(p, m));
-                if (F32) q = fmaxf(q, __shfl_xor(q, m));
-            }
+            p = neighbours_max<F32 ? 16 : 8>(p);
+            if (F32) q = neighbours_max<16>(q);
             if (F32) {
                 if ((lane & 15) == 0) {
                     seg[(j - j0) * PER + (lane >> 4)] = p;
@@ -387,7 +452,14 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
         __syncthreads();
         if (!last_one) return;
         if constexpr (TOP)
-            for (int i = threadIdx.x; i < segments; i += kThreads) seg[i] = __hip_atomic_load(row_seg + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int base = threadIdx.x; base < segments; base += 8 * kThreads) {
+                float in[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) in[i] = __hip_atomic_load(row_seg + min(base + i * kThreads, segments - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (base + i * kThreads < segments) seg[base + i * kThreads] = in[i];
+            }
         r = row_sums{-INFINITY, kHuge, 0.f, 0.f};
         if ((int)threadIdx.x < a.parts) {
             const float* p = a.sums + ((size_t)row * a.parts + threadIdx.x) * 4;
