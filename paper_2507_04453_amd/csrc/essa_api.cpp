@@ -1031,7 +1031,7 @@ extern "C" essa_status essa_token_logprobs(essa_ctx* ctx, const void* logits, in
     if (R < essa_k::kLogprobSplitRows && !ctx->counts) {
         if (ctx->capturing) return essa_fail(ESSA_ERR_STATE, "%s: its first call makes its counts: run it once before essa_graph_begin", who);
         void* p = nullptr;
-        const size_t bytes = essa_k::kLogprobSplitRows * sizeof(int32_t);
+        const size_t bytes = essa_k::kLogprobSplitRows * essa_k::kLogprobCountStep * sizeof(int32_t);
         const hipError_t e = device_alloc(&p, bytes);
         if (e != hipSuccess) return essa_fail(ESSA_ERR_OOM, "%s: hipMalloc of %zu bytes: %s", who, bytes, hipGetErrorString(e));
         ctx->counts = (int32_t*)p;

@@ -38,7 +38,7 @@ struct essa_ctx {
     std::vector<struct essa_graph*> graphs;   // recorded graphs that are still alive: their launches hold pointers into ws
     void* told_at = nullptr;   // 64 bytes of page-locked host memory and an event, both or neither: what the steps of a refresh tell the host
     hipEvent_t told = nullptr;
-    int32_t* counts = nullptr; // [kLogprobSplitRows] counts of finished parts of a row, 0 between calls (made by the first call that wants them)
+    int32_t* counts = nullptr; // [kLogprobSplitRows, kLogprobCountStep] counts of finished parts of a row, 0 between calls (made by the first call that wants them)
 };
 struct essa_graph {
     essa_ctx* ctx = nullptr;   // null once the context is gone: the graph can then only be destroyed

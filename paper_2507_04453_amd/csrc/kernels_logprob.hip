@@ -14,7 +14,6 @@ namespace {
 using essa_k::kLogprobSegment;
 using essa_k::logprob_args;
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kVec = 8;                        // values of a lane's load (two loads in fp32)
 constexpr int kLoad = 64 * kVec;               // values of a wave's
 constexpr float kSlack = 8.f;
@@ -89,36 +88,39 @@ __device__ __forceinline__ void unpack(const row_view<F32>& v, int j, int lane, 
     }
 }
 
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x = fmaxf(x, __shfl_xor(x, m));
-    return x;
-}
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-    return x;
-}
-// over a lane's 8 or 16 neighbours, without a trip through LDS
-template <int N>
-__device__ __forceinline__ float neighbours_max(float x) {
-#define STEP(ctrl) x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl, 0xf, 0xf, true)))
+// Over a lane's N neighbours (16, 32 or all 64), without a trip through LDS; every one of them gets the result.
+template <int N, class Op>
+__device__ __forceinline__ float neighbours(float x, Op op) {
+#define STEP(ctrl) x = op(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl, 0xf, 0xf, true)))
     STEP(0xb1);                                                // quad_perm 1 0 3 2
     STEP(0x4e);                                                // quad_perm 2 3 0 1
     STEP(0x141);                                               // row_half_mirror
-    if (N == 16) STEP(0x140);                                  // row_mirror
+    STEP(0x140);                                               // row_mirror
 #undef STEP
+    if (N >= 32) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    }
+    if (N == 64) {
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
     return x;
 }
+template <int N>
+__device__ __forceinline__ float neighbours_max(float x) { return neighbours<N>(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_max(float x) { return neighbours_max<64>(x); }
+__device__ __forceinline__ float wave_sum(float x) { return neighbours<64>(x, [](float a, float b) { return a + b; }); }
 // all threads' sums as one, everywhere; waves: LDS
-__device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
+template <int W>
+__device__ void join_threads(row_sums& a, float k, float (&waves)[3][W]) {
     const int wave = threadIdx.x / 64;
     const float max = wave_max(a.max);
     if ((threadIdx.x & 63) == 0) waves[0][wave] = max;
     __syncthreads();
     a.max = waves[0][0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) a.max = fmaxf(a.max, waves[0][w]);
+    for (int w = 1; w < W; ++w) a.max = fmaxf(a.max, waves[0][w]);
     move_to(a, down_of(a.max, k));
     const float s = wave_sum(a.s), t = wave_sum(a.t);
     if ((threadIdx.x & 63) == 0) {
@@ -128,7 +130,7 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
     __syncthreads();
     a.s = a.t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         a.s += waves[1][w];
         a.t += waves[2][w];
     }
@@ -139,47 +141,85 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[3][kWaves]) {
 // The n_top largest of a row.  A segment is kLogprobSegment consecutive values, of which `seg` (LDS) holds the largest.  With segments ordered by
 // it, the earlier of equal ones first, the n_top largest values lie in the n_top first segments: a value outside of them has one in each
 // in front of it.  So a few segments are read again, and of them what is not below a limit that n_top values reach is put in order.
-// The limit is the n_top-th largest of the threads' own segments' largest (upper half of the bits: a little less): 256 numbers instead of
+// The limit is the n_top-th largest of the largest of 64 or 256 shares of the segments (upper half of the bits: a little less): few numbers instead of
 // thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
-// segments themselves are found, bit by bit; where too many values do, they are taken one after another.
+// segments themselves are found, bit by bit.  Where too many of their values reach the limit, a higher one comes from the largest of every thread's share of
+// those; where still too many do, they are taken one after another.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSegments = 256, kCandidates = 512;
+template <int T>
 struct top_lds {
-    uint32_t best[kThreads];
-    int counts[2][3][kWaves];
+    uint32_t best[T];
+    int counts[2][3][T / 64];
     int list[kSegments];
     unsigned long long keys[kCandidates];
     int segments, found;
-    unsigned long long most[kWaves];
+    unsigned long long most[T / 64];
 };
-// The largest number with at least `want` of a wave's keys (N a lane) at or above it and `bits` upper bits.
+// The largest number of 16 upper bits with at least `want` of a wave's keys (N a lane) at or above it, two bits at a time.
 template <int N>
-__device__ __forceinline__ uint32_t limit_of(const uint32_t (&key)[N], int want, int bits) {
+__device__ __forceinline__ uint32_t limit_of(const uint32_t (&key)[N], int want) {
     uint32_t limit = 0;
-    for (int bit = 31; bit >= 32 - bits; --bit) {
-        const uint32_t tried = limit | 1u << bit;
-        int count = 0;
+    for (int bit = 30; bit >= 16; bit -= 2) {
+        int count[3];
 #pragma unroll
-        for (int i = 0; i < N; ++i) count += __popcll(__ballot(key[i] >= tried));
-        if (count >= want) {
-            limit = tried;
-            if (count == want) break;
+        for (int k = 0; k < 3; ++k) {
+            const uint32_t tried = limit | (uint32_t)(k + 1) << bit;
+            count[k] = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) count[k] += __popcll(__ballot(key[i] >= tried));
         }
+        limit |= (count[2] >= want ? 3u : count[1] >= want ? 2u : count[0] >= want ? 1u : 0u) << bit;
     }
     return limit;
 }
+// the same of all threads' keys; l.best is this call's
+template <int T>
+__device__ uint32_t limit_of_threads(uint32_t key, int want, top_lds<T>& l) {
+    const int lane = threadIdx.x & 63;
+    l.best[threadIdx.x] = key;
+    __syncthreads();
+    // (every wave finds the same)
+    uint32_t mine[T / 64];
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) mine[i] = l.best[64 * i + lane];
+    if (want > 32) return limit_of(mine, want);
+#pragma unroll
+    for (int i = 1; i < T / 64; ++i) mine[0] = max(mine[0], mine[i]);
+    const uint32_t one[1] = {mine[0]};
+    return limit_of(one, want);
+}
+// places[i] for those of a lane's N numbers that are `in`: one atomic a wave
+template <int N>
+__device__ __forceinline__ void places(int* count, const bool (&in)[N], int (&place)[N]) {
+    const int lane = threadIdx.x & 63;
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const unsigned long long has = __ballot(in[i]);
+        place[i] = total + __popcll(has & ((1ull << lane) - 1));
+        total += __popcll(has);
+    }
+    if (total == 0) return;
+    int first = 0;
+    if (lane == 0) first = atomicAdd(count, total);
+    first = __builtin_amdgcn_readfirstlane(first);
+#pragma unroll
+    for (int i = 0; i < N; ++i) place[i] += first;
+}
 // The `want` first segments into l.list: returns the limit that parts them from the rest.
-template <bool F32>
-__device__ __attribute__((noinline)) uint32_t first_segments(const float* seg, int segments, int want, top_lds& l) {
+template <bool F32, int T>
+__device__ uint32_t first_segments(const float* seg, int segments, int want, top_lds<T>& l) {
+    constexpr int WAVES = T / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, whole = (segments + 63) & ~63;
     const auto count_from = [&](uint32_t from, int slot) {
         int count = 0;
-        for (int i = threadIdx.x; i < whole; i += kThreads) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= from));
+        for (int i = threadIdx.x; i < whole; i += T) count += __popcll(__ballot(i < segments && ordered(seg[min(i, segments - 1)]) >= from));
         if (lane == 0) l.counts[slot & 1][0][wave] = count;
         __syncthreads();
         count = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) count += l.counts[slot & 1][0][w];
+        for (int w = 0; w < WAVES; ++w) count += l.counts[slot & 1][0][w];
         return count;
     };
     uint32_t limit = 0;                                        // (bf16: the lower half of a key says nothing about its order)
@@ -190,7 +230,7 @@ __device__ __attribute__((noinline)) uint32_t first_segments(const float* seg, i
     __syncthreads();
     // those above it, and the first ones of those at it
     int at_above = 0, equal = 0;
-    for (int base = 0, turn = 0; base < segments; base += kThreads, turn ^= 1) {
+    for (int base = 0, turn = 0; base < segments; base += T, turn ^= 1) {
         const int i = base + (int)threadIdx.x;
         const uint32_t key = i < segments ? ordered(seg[i]) : 0u;
         const bool gt = i < segments && key >= next, eq = i < segments && key >= limit && key < next;
@@ -202,7 +242,7 @@ __device__ __attribute__((noinline)) uint32_t first_segments(const float* seg, i
         __syncthreads();
         int my_above = at_above + __popcll(g & below), my_equal = equal + __popcll(e & below);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             if (w < wave) {
                 my_above += l.counts[turn][1][w];
                 my_equal += l.counts[turn][2][w];
@@ -216,44 +256,45 @@ __device__ __attribute__((noinline)) uint32_t first_segments(const float* seg, i
     __syncthreads();
     return limit;
 }
-// put(rank, index, value): the result's places, all of them.  wave-wide appends: at most one atomic a wave
-__device__ __forceinline__ int places(int* count, bool mine) {
-    const int lane = threadIdx.x & 63;
-    const unsigned long long has = __ballot(mine);
-    int first = 0;
-    if (lane == 0 && has) first = atomicAdd(count, __popcll(has));
-    return __builtin_amdgcn_readfirstlane(first) + __popcll(has & ((1ull << lane) - 1));
-}
-template <bool F32, class Put>
-__device__ void find_top(const row_view<F32>& v, const float* seg, int segments, int n_top, top_lds& l, Put put) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, want = min(n_top, segments);
-    {
-        float best = -INFINITY;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < segments; i += kThreads) best = fmaxf(best, seg[i]);
-        l.best[threadIdx.x] = (int)threadIdx.x < segments ? ordered(best) : 0u;
-        if (threadIdx.x == 0) l.segments = l.found = 0;
-    }
-    __syncthreads();
-    uint32_t mine[kThreads / 64];
+// put(rank, index, value): the result's places, all of them
+template <bool F32, int T, class Put>
+__device__ void find_top(const row_view<F32>& v, const float* seg, int segments, int n_top, top_lds<T>& l, Put put) {
+    constexpr int WAVES = T / 64, PER = F32 ? 4 : 8, LOADS = kLogprobSegment / PER;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    // segments
+    constexpr int HOLD = T == 64 ? 1 : 1536 / T;               // of a thread, as many as its vocabularies have, or nearly
+    float held[HOLD], best = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) mine[i] = l.best[64 * i + lane];
-    uint32_t limit = limit_of(mine, want, 16);                 // (every wave finds the same)
-    const int whole = (segments + 63) & ~63;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < whole; i += kThreads) {
-        const bool in = i < segments && ordered(seg[min(i, segments - 1)]) >= limit;
-        if (__any(in)) {
-            const int at = places(&l.segments, in);
-            if (in && at < kSegments) l.list[at] = i;
+    for (int i = 0; i < HOLD; ++i) {
+        const int at = threadIdx.x + i * T;
+        held[i] = seg[min(at, segments - 1)];
+        best = fmaxf(best, at < segments ? held[i] : -INFINITY);
+    }
+    for (int at = threadIdx.x + HOLD * T; at < segments; at += T) best = fmaxf(best, seg[at]);
+    if (threadIdx.x == 0) l.segments = l.found = 0;
+    uint32_t limit = limit_of_threads<T>((int)threadIdx.x < segments ? ordered(best) : 0u, n_top, l);
+    if (segments < n_top) limit = 0;                           // a largest of each is not enough
+    for (int base = 0; base < segments; base += HOLD * T) {
+        bool in[HOLD];
+        int place[HOLD];
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i) {
+            const int at = base + (int)threadIdx.x + i * T;
+            const float x = base == 0 ? held[i] : seg[min(at, segments - 1)];
+            in[i] = at < segments && ordered(x) >= limit;
         }
+        places<HOLD>(&l.segments, in, place);
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i)
+            if (in[i] && place[i] < kSegments) l.list[place[i]] = base + threadIdx.x + i * T;
     }
     __syncthreads();
     int chosen = l.segments;
     if (chosen > kSegments) {
-        limit = first_segments<F32>(seg, segments, want, l);
-        chosen = want;
+        limit = first_segments<F32, T>(seg, segments, n_top, l);
+        chosen = n_top;
     }
+    // their values
     const auto key_of = [&](int at, float x) -> unsigned long long {           // of value `at` of the row; 0: none
         const uint32_t key = ordered(x);
         return at >= v.skip && at < v.n && x > -INFINITY && key >= limit ? (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)(at - v.skip)) : 0;
@@ -262,65 +303,101 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
         const uint32_t b = (uint32_t)(key >> 32);
         return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
     };
-    constexpr int PER = F32 ? 4 : 8, LOADS = kLogprobSegment / PER;            // of 16 bytes
-    for (int i = threadIdx.x; i < ((chosen * LOADS + 63) & ~63); i += kThreads) {
-        const bool real = i < chosen * LOADS;
-        const int first = l.list[real ? i / LOADS : 0] * kLogprobSegment + i % LOADS * PER;
-        const u32x4 w = *(const u32x4*)(v.at + (size_t)min(first, (v.n - 1) & ~(PER - 1)) * (F32 ? 4 : 2));
+    const auto each_load = [&](auto use) {                     // use(keys of the 16 bytes): whole waves
+        for (int i = threadIdx.x; i < ((chosen * LOADS + 63) & ~63); i += T) {
+            const bool real = i < chosen * LOADS;
+            const int first = l.list[real ? i / LOADS : 0] * kLogprobSegment + i % LOADS * PER;
+            const u32x4 w = *(const u32x4*)(v.at + (size_t)min(first, (v.n - 1) & ~(PER - 1)) * (F32 ? 4 : 2));
+            unsigned long long key[PER];
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const float x = __uint_as_float(F32 ? w[k & 3] : k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
-            const unsigned long long key = real ? key_of(first + k, x) : 0;
-            if (__any(key != 0)) {
-                const int at = places(&l.found, key != 0);
-                if (key && at < kCandidates) l.keys[at] = key;
+            for (int k = 0; k < PER; ++k) {
+                const float x = __uint_as_float(F32 ? w[k & 3] : k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+                key[k] = real ? key_of(first + k, x) : 0;
             }
+            use(key);
         }
+    };
+    const auto collect = [&] {
+        each_load([&](const unsigned long long (&key)[PER]) {
+            bool in[PER];
+            int place[PER];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) in[k] = key[k] != 0;
+            places<PER>(&l.found, in, place);
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (in[k] && place[k] < kCandidates) l.keys[place[k]] = key[k];
+        });
+        __syncthreads();
+        return l.found;
+    };
+    int found = limit || chosen * kLogprobSegment <= kCandidates ? collect() : kCandidates + 1;
+    if (found > kCandidates) {
+        uint32_t mine = 0;
+        each_load([&](const unsigned long long (&key)[PER]) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) mine = max(mine, (uint32_t)(key[k] >> 32));
+        });
+        __syncthreads();                                       // everybody has the count
+        if (threadIdx.x == 0) l.found = 0;
+        limit = max(limit, limit_of_threads<T>(mine, n_top, l));
+        found = collect();
     }
-    __syncthreads();
-    const int found = l.found;
     if (found <= kCandidates) {
-        for (int i = threadIdx.x; i < found; i += kThreads) {
+        for (int i = threadIdx.x; i < found; i += T) {
             const unsigned long long key = l.keys[i];
             int rank = 0;
 #pragma unroll 8
             for (int o = 0; o < found; ++o) rank += l.keys[o] > key;
             if (rank < n_top) put(rank, (int)(0xffffffffu - (uint32_t)key), value_of(key));
         }
-        for (int i = found + threadIdx.x; i < n_top; i += kThreads) put(i, -1, -INFINITY);
+        for (int i = found + threadIdx.x; i < n_top; i += T) put(i, -1, -INFINITY);
         return;
     }
     unsigned long long last = ~0ull;
     for (int rank = 0; rank < n_top; ++rank) {
-        unsigned long long best = 0;
-        for (int i = threadIdx.x; i < chosen * kLogprobSegment; i += kThreads) {
-            const int at = l.list[i / kLogprobSegment] * kLogprobSegment + i % kLogprobSegment;
-            const unsigned long long key = key_of(at, v.value(min(at, v.n - 1)));
-            if (key < last && key > best) best = key;
-        }
+        unsigned long long most = 0;
+        each_load([&](const unsigned long long (&key)[PER]) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) most = key[k] < last && key[k] > most ? key[k] : most;
+        });
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
-            const unsigned long long o = __shfl_xor(best, m);
-            best = o > best ? o : best;
+            const unsigned long long o = __shfl_xor(most, m);
+            most = o > most ? o : most;
         }
-        if (lane == 0) l.most[wave] = best;
+        if (lane == 0) l.most[wave] = most;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) best = l.most[w] > best ? l.most[w] : best;
+        for (int w = 0; w < WAVES; ++w) most = l.most[w] > most ? l.most[w] : most;
         __syncthreads();
-        if (threadIdx.x == 0) put(rank, best ? (int)(0xffffffffu - (uint32_t)best) : -1, best ? value_of(best) : -INFINITY);
-        last = best;
+        if (threadIdx.x == 0) put(rank, most ? (int)(0xffffffffu - (uint32_t)most) : -1, most ? value_of(most) : -INFINITY);
+        last = most;
     }
 }
 
-// What a row gives, once its sums are whole.  A row of huge numbers (all of its values the type's lowest, say) is summed again here,
-// as 2^(k (x - max)).
-template <bool F32, bool TOP>
-__device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, const float* seg, int segments, float (&waves)[3][kWaves], top_lds* l) {
+// A given token's logit; a number that no row holds where there is none (padding: 0, past V: 1).
+struct given {
+    float x;
+    int what;                  // 2: x
+};
+template <bool F32>
+__device__ __forceinline__ given given_of(const logprob_args& a, const row_view<F32>& v, int row, int i) {
+    given g{0.f, 0};
+    if (i < a.n_tokens) {
+        const int token = a.tokens[(size_t)row * a.n_tokens + i];
+        g.what = token < 0 ? 0 : token < a.V ? 2 : 1;
+        g.x = v.value(v.skip + (g.what == 2 ? token : 0));
+    }
+    return g;
+}
+template <bool F32, bool TOP, int T>
+__device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, given first, const float* seg, int segments, float (&waves)[3][T / 64],
+                           top_lds<T>* l) {
     const bool huge = fabsf(r.max) <= 3.402823466e38f && !(fabsf(r.max * a.k) <= kHuge);
     if (huge) {
         row_sums mine{r.max, 0.f, 0.f, 0.f};
-        for (int i = v.skip + (int)threadIdx.x; i < v.n; i += kThreads) {
+        for (int i = v.skip + (int)threadIdx.x; i < v.n; i += T) {
             const float d = (v.value(i) - r.max) * a.k, e = __builtin_amdgcn_exp2f(d);
             mine.s += e;
             mine.t = fmaf(e, fmaxf(d, -256.f), mine.t);
@@ -334,7 +411,7 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
         __syncthreads();
         r.s = r.t = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < T / 64; ++w) {
             r.s += waves[1][w];
             r.t += waves[2][w];
         }
@@ -349,34 +426,34 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
         if (nothing || x == -INFINITY) return -INFINITY;
         return fmaf(x - r.max, a.scale, most);
     };
-    for (int i = threadIdx.x; i < a.n_tokens; i += kThreads) {
-        const size_t at = (size_t)row * a.n_tokens + i;
-        const int token = a.tokens[at];
-        a.logp[at] = token < 0 ? 0.f : token < a.V ? logp(v.value(v.skip + token)) : __uint_as_float(0x7fc00000u);
+    for (int i = threadIdx.x; i < a.n_tokens; i += T) {
+        const given g = i < T ? first : given_of<F32>(a, v, row, i);
+        a.logp[(size_t)row * a.n_tokens + i] = g.what == 0 ? 0.f : g.what == 2 ? logp(g.x) : __uint_as_float(0x7fc00000u);
     }
     if (a.entropy && threadIdx.x == 0) a.entropy[row] = bad ? __uint_as_float(0x7fc00000u) : nothing ? 0.f : (log_s - r.t / r.s) * kLn2;
     if constexpr (TOP) {
         int32_t* ids = a.top_ids + (size_t)row * a.n_top;
         float* lps = a.top_logp + (size_t)row * a.n_top;
         if (nothing || bad) {
-            for (int i = threadIdx.x; i < a.n_top; i += kThreads) {
+            for (int i = threadIdx.x; i < a.n_top; i += T) {
                 ids[i] = -1;
                 lps[i] = logp(-INFINITY);
             }
             return;
         }
-        find_top<F32>(v, seg, segments, a.n_top, *l, [&](int rank, int index, float x) {
+        find_top<F32, T>(v, seg, segments, a.n_top, *l, [&](int rank, int index, float x) {
             ids[rank] = index;
             lps[rank] = logp(x);
         });
     }
 }
 
-template <bool F32, bool TOP>
-__global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a) {
+template <bool F32, bool TOP, int T>
+__global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
     extern __shared__ float seg[];                             // [segments of this part], then of the row
-    __shared__ float waves[3][kWaves];
-    __shared__ top_lds top;
+    constexpr int W = T / 64;
+    __shared__ float waves[3][W];
+    __shared__ top_lds<T> top;
     __shared__ int last_one;
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     const row_view<F32> v(a, row);
@@ -384,6 +461,7 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
     const int j0 = part * per + min(part, more), j1 = j0 + per + (part < more);
     constexpr int PER = kLoad / kLogprobSegment;               // segments of a load
 
+    const given first = given_of<F32>(a, v, row, threadIdx.x);                 // asked for before the row, or they would be waited for at the end
     row_sums r{-INFINITY, kHuge, 0.f, 0.f};
     const auto take = [&](int j, const raw_values<F32>& raw) {
         float x[kVec];
@@ -394,16 +472,17 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
             most = fmaxf(most, x[i]);
             half = fmaxf(half, x[4 + i]);
         }
-        if constexpr (TOP) {                                   // a segment is eight lanes' (fp32: sixteen lanes' of a half)
-            float p = F32 ? most : fmaxf(most, half), q = half;
-            p = neighbours_max<F32 ? 16 : 8>(p);
-            if (F32) q = neighbours_max<16>(q);
+        if constexpr (TOP) {                                   // a segment is sixteen lanes' (fp32: 32 lanes' of a half)
             if (F32) {
-                if ((lane & 15) == 0) {
-                    seg[(j - j0) * PER + (lane >> 4)] = p;
-                    seg[(j - j0) * PER + 4 + (lane >> 4)] = q;
+                const float p = neighbours_max<32>(most), q = neighbours_max<32>(half);
+                if ((lane & 31) == 0) {
+                    seg[(j - j0) * PER + (lane >> 5)] = p;
+                    seg[(j - j0) * PER + 2 + (lane >> 5)] = q;
                 }
-            } else if ((lane & 7) == 0) seg[(j - j0) * PER + (lane >> 3)] = p;
+            } else {
+                const float p = neighbours_max<16>(fmaxf(most, half));
+                if ((lane & 15) == 0) seg[(j - j0) * PER + (lane >> 4)] = p;
+            }
         }
         most = fmaxf(most, half);
         r.max = fmaxf(r.max, most);
@@ -419,13 +498,13 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
     };
     raw_values<F32> raw[4];
     int j = j0 + wave;
-    for (; j + 3 * kWaves < j1; j += 4 * kWaves) {
+    for (; j + 3 * W < j1; j += 4 * W) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_values<F32>(v, j + i * kWaves, lane, raw[i]);
+        for (int i = 0; i < 4; ++i) load_values<F32>(v, j + i * W, lane, raw[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) take(j + i * kWaves, raw[i]);
+        for (int i = 0; i < 4; ++i) take(j + i * W, raw[i]);
     }
-    for (; j < j1; j += kWaves) {
+    for (; j < j1; j += W) {
         load_values<F32>(v, j, lane, raw[0]);
         take(j, raw[0]);
     }
@@ -440,26 +519,17 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
         }
         float* row_seg = a.segments + (size_t)row * a.row_segments;
         if constexpr (TOP)
-            for (int i = threadIdx.x; i < (j1 - j0) * PER; i += kThreads) __hip_atomic_store(row_seg + j0 * PER + i, seg[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            for (int i = threadIdx.x; i < (j1 - j0) * PER; i += T) __hip_atomic_store(row_seg + j0 * PER + i, seg[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // written through; once all waves' stores have been acknowledged the count may say so, and the last part finishes the row
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) {
-            const bool last = __hip_atomic_fetch_add(a.done + row, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.parts - 1;
-            if (last) __hip_atomic_store(a.done + row, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const bool last = __hip_atomic_fetch_add(a.done + row * essa_k::kLogprobCountStep, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.parts - 1;
+            if (last) __hip_atomic_store(a.done + row * essa_k::kLogprobCountStep, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             last_one = last;
         }
         __syncthreads();
         if (!last_one) return;
-        if constexpr (TOP)
-            for (int base = threadIdx.x; base < segments; base += 8 * kThreads) {
-                float in[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) in[i] = __hip_atomic_load(row_seg + min(base + i * kThreads, segments - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (base + i * kThreads < segments) seg[base + i * kThreads] = in[i];
-            }
         r = row_sums{-INFINITY, kHuge, 0.f, 0.f};
         if ((int)threadIdx.x < a.parts) {
             const float* p = a.sums + ((size_t)row * a.parts + threadIdx.x) * 4;
@@ -468,9 +538,18 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
             r.t = __hip_atomic_load(p + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             r.down = down_of(r.max, a.k);
         }
+        if constexpr (TOP)
+            for (int base = threadIdx.x; base < segments; base += 8 * T) {
+                float in[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) in[i] = __hip_atomic_load(row_seg + min(base + i * T, segments - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (base + i * T < segments) seg[base + i * T] = in[i];
+            }
         join_threads(r, a.k, waves);
     }
-    finish_row<F32, TOP>(a, v, row, r, seg, segments, waves, &top);
+    finish_row<F32, TOP, T>(a, v, row, r, first, seg, segments, waves, &top);
 }
 
 }  // namespace
@@ -478,26 +557,42 @@ __global__ __launch_bounds__(kThreads) void token_logprobs_kernel(logprob_args a
 namespace essa_k {
 
 static int loads_of(int V, int x_dtype) { return (V + (x_dtype == ESSA_F32 ? 3 : 7) + kLoad - 1) / kLoad; }
-// Parts of a row: enough workgroups for the chip, each with some loads a wave.
-static int parts_of(int R, int V, int x_dtype) {
-    const int loads = loads_of(V, x_dtype), most = std::min(kThreads, std::max(1, loads / (2 * kWaves)));
-    return R >= kLogprobSplitRows ? 1 : std::max(1, std::min(most, 1024 / R));
+// Threads of a workgroup, and workgroups a row.  One wave does a row of few loads (8192 rows of 1000 below); where rows are about as many as CUs one large
+// workgroup each spares the parts' joining; fewer rows are shared, so that the chip has two workgroups a CU; many rows of a large vocabulary
+// run a little better with eight waves than with four.  us with 256 threads and up to 1024 workgroups, 512 and 512, 1024 and one a row: 256 rows of 152064 with 20 of
+// them 26.5, 24.7, 22.7; 160 with 5 19.2, 18.5, 19.9; 64 with 5 13.1, 13.1, 13.4; 400 with 8 37.0, 33.4, 39.5, but 300 with 5 28.2, 32.5, 37.5; 2048 with 20
+// 127, 120, 160; 4096 of 32000 with 20 64.7, 71.7, 132.
+struct shape {
+    int threads, parts;
+};
+static shape shape_of(int R, int V, int x_dtype) {
+    const int loads = loads_of(V, x_dtype);
+    if (loads <= 8) return {64, 1};
+    if (R >= kLogprobSplitRows) return {loads >= 128 ? 512 : 256, 1};
+    if (R > 192 && R <= 256) return {1024, 1};
+    return {512, std::max(1, std::min({256, loads / 8, 512 / R}))};
 }
 size_t token_logprobs_bytes(int R, int V, int x_dtype, int n_top) {
-    const int parts = parts_of(R, V, x_dtype);
+    const int parts = shape_of(R, V, x_dtype).parts;
     return parts > 1 ? (size_t)R * (parts * 4 + (n_top ? loads_of(V, x_dtype) * (kLoad / kLogprobSegment) : 0)) * sizeof(float) : 0;
 }
 
+template <int T>
+static void launch(hipStream_t st, const logprob_args& a, int x_dtype, int R) {
+    const size_t lds = a.n_top ? (size_t)a.row_segments * sizeof(float) : 0;
+    const auto kernel = x_dtype == ESSA_F32 ? a.n_top ? token_logprobs_kernel<true, true, T> : token_logprobs_kernel<true, false, T>
+                                            : a.n_top ? token_logprobs_kernel<false, true, T> : token_logprobs_kernel<false, false, T>;
+    kernel<<<R * a.parts, T, lds, st>>>(a);
+}
+
 hipError_t token_logprobs(hipStream_t st, logprob_args a, int x_dtype, int R, int32_t* done, void* ws) {
-    a.parts = parts_of(R, a.V, x_dtype);
+    const shape how = shape_of(R, a.V, x_dtype);
+    a.parts = how.parts;
     a.row_segments = loads_of(a.V, x_dtype) * (kLoad / kLogprobSegment);
     a.done = done;
     a.sums = (float*)ws;
     a.segments = a.sums + (size_t)R * a.parts * 4;
-    const size_t lds = a.n_top ? (size_t)a.row_segments * sizeof(float) : 0;
-    const auto kernel = x_dtype == ESSA_F32 ? a.n_top ? token_logprobs_kernel<true, true> : token_logprobs_kernel<true, false>
-                                            : a.n_top ? token_logprobs_kernel<false, true> : token_logprobs_kernel<false, false>;
-    kernel<<<R * a.parts, kThreads, lds, st>>>(a);
+    (how.threads == 64 ? launch<64> : how.threads == 256 ? launch<256> : how.threads == 512 ? launch<512> : launch<1024>)(st, a, x_dtype, R);
     return hipGetLastError();
 }
 

@@ -75,7 +75,8 @@ def _tokens(R, V, n, seed):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("R,V,n,top", [
     (1, 1, 1, 1), (3, 2, 2, 64), (2, 7, 1, 5), (5, 64, 3, 3), (1, 65, 1, 64), (4, 511, 1, 8), (2, 512, 1, 0), (3, 513, 2, 20), (1, 4095, 1, 5), (7, 4097, 16, 1),
-    (2, 32001, 4, 64), (1, 152064, 1, 5), (300, 1000, 1, 3), (40, 20011, 2, 20), (600, 515, 1, 7), (1, 524288, 1, 2),
+    (2, 32001, 4, 64), (1, 152064, 1, 5), (300, 1000, 1, 3), (40, 20011, 2, 20), (600, 515, 1, 7), (1, 524288, 1, 2), (4, 511, 1, 64), (3, 513, 1, 63), (600, 900, 1, 64), (2, 4000, 1, 64), (2, 8200, 1, 64),
+    (3, 8192, 1, 33), (2, 300001, 1, 40), (600, 8001, 1, 32), (200, 5000, 1, 9), (256, 20011, 1, 64), (193, 70001, 2, 5), (520, 66000, 1, 5), (515, 4100, 1, 64), (257, 9000, 1, 3),
 ])
 def test_sizes(essa, ctx, dtype, R, V, n, top):
     x, view = _logits(R, V, dtype, 1)
@@ -99,7 +100,7 @@ def test_temperatures(essa, ctx, dtype, scale):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("R", [2, 520])
+@pytest.mark.parametrize("R", [2, 520, 200])
 def test_sharp_and_flat_rows(essa, ctx, dtype, R):
     """One certain token, equal logits, logits far from zero, rising ones (every lane's maximum moves all the time)."""
     def edit(x):
@@ -114,7 +115,7 @@ def test_sharp_and_flat_rows(essa, ctx, dtype, R):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("R,V", [(4, 700), (4, 40000), (515, 3000)])
+@pytest.mark.parametrize("R,V", [(4, 700), (4, 40000), (515, 3000), (515, 6000), (200, 40000), (515, 66000)])
 def test_equal_logits_come_in_order(essa, ctx, dtype, R, V):
     """Few levels, so that almost everything is a tie: the lower tokens are taken, and -0 equals 0."""
     def edit(x):
@@ -131,7 +132,7 @@ def test_equal_logits_come_in_order(essa, ctx, dtype, R, V):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("R,V", [(12, 900), (12, 30000), (520, 600)])
+@pytest.mark.parametrize("R,V", [(12, 900), (12, 30000), (520, 600), (520, 6000), (200, 30000), (515, 66000)])
 def test_forbidden_tokens(essa, ctx, dtype, R, V):
     """-inf: most of a row, all but a few, all of it.  The type's lowest value is a value, in part of a row or all over it."""
     low = float(torch.finfo(dtype).min)
@@ -163,7 +164,7 @@ def test_forbidden_tokens(essa, ctx, dtype, R, V):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("R,V", [(8, 1000), (8, 20000), (520, 600)])
+@pytest.mark.parametrize("R,V", [(8, 1000), (8, 20000), (520, 600), (520, 6000), (200, 20000)])
 def test_rows_that_are_not_finite(essa, ctx, dtype, R, V):
     """A NaN of either sign or a +inf anywhere makes its row NaN and no other."""
     def edit(x):
