@@ -2,6 +2,7 @@
 #include <hip/hip_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kv_device.h"
 
@@ -98,6 +99,10 @@ constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
 // 115 and 112 (33000); 64 x 36 behind 264 56 and 44 (16000); 64 x 36 behind 2000 182 and 143 (70000).  Between 8000 and 30000
 // either may be ahead, by up to a third.
 constexpr int kLittle = 8192;
+// Masks: calls of little work in units of kNarrow columns, where every wave takes a block in four, instead of 64, where each takes all of them: more units to
+// share, and a quarter of the steps one after another.  Trees of 26 rows (28 heads on 4), us with 64 and with 16: one of 500 tokens (of 16 rows) 28, 14; 8 of 1000 44, 23;
+// 16 of 1000 46, 30; fp32 (8 heads of 64, 63 rows) one of 600 43, 17, but 64 of them, 12800 long, 74 and 90.
+constexpr int kNarrow = 16;
 
 // With sinks (MASK) the blocks that hold them come first and lo more are left out behind them: block i of an entry's is i, or lo + i from sink_blocks on.
 template <bool MASK>
@@ -106,12 +111,12 @@ struct entry_span {            // the blocks that an entry's rows see, and how m
     int lo, n, groups;
 };
 template <bool MASK>
-__device__ __forceinline__ entry_span span_of(const attn_args& a, int len, int rows) {
+__device__ __forceinline__ entry_span span_of(const attn_args& a, int len, int rows, int width = kColumns) {
     entry_span s;
     const int lo = a.window > 0 ? max(len - rows - a.window + 1, 0) : 0;
     s.lo = left_out<MASK>(lo / kKvBlock, a.sink_blocks);
     s.n = rows > 0 && len > 0 ? (len + kKvBlock - 1) / kKvBlock - s.lo : 0;
-    s.groups = (int)(((unsigned)(rows * a.g) + kColumns - 1) / kColumns);      // R rows of q_heads are below 2^31
+    s.groups = (int)(((unsigned)(rows * a.g) + width - 1) / width);            // R rows of q_heads are below 2^31
     return s;
 }
 
@@ -121,6 +126,7 @@ struct attn_list {
     int2 *who, *rows;          // [n] slot and len; row0 and rows (null: one row each)
     int even;                  // > 0: every unit counts as this long
     bool prompts;              // entries of many rows are the prompt kernel's
+    int width;                 // columns of a unit
     bool blank;                // there are entries of more than kBlank rows that see nothing
     __device__ __forceinline__ int4 entry(int b) const {
         const int2 w = who[b], r = rows ? rows[b] : int2{b, 1};
@@ -139,8 +145,8 @@ template <bool F32, bool OWN_ROWS, bool MASK>
 __device__ attn_list make_list(const attn_args& a, void* lds) {                // 256 threads
     __shared__ int waves[5][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
-    attn_list l{(int*)((int2*)lds + (OWN_ROWS ? 2 * n : n)), (int2*)lds, OWN_ROWS ? (int2*)lds + n : nullptr, 0, false, false};
-    if (OWN_ROWS && !F32 && a.tiles) {                                     // every workgroup finds the same
+    attn_list l{(int*)((int2*)lds + (OWN_ROWS ? 2 * n : n)), (int2*)lds, OWN_ROWS ? (int2*)lds + n : nullptr, 0, false, kColumns, false};
+    if (OWN_ROWS && ((!F32 && a.tiles) || MASK)) {                         // every workgroup finds the same
         int work = 0;
         for (int b = lo; b < hi; ++b) {
             const kv_entry e = kv_entry_of(a.v, a.rows, b);
@@ -150,13 +156,15 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
         work = wave_scan(work, [](int x, int y) { return x + y; });
         if ((threadIdx.x & 63) == 63) waves[0][threadIdx.x / 64] = work;
         lds_barrier();
-        l.prompts = uniform(waves[0][0] + waves[0][1] + waves[0][2] + waves[0][3]) > kLittle;
+        work = uniform(waves[0][0] + waves[0][1] + waves[0][2] + waves[0][3]);
+        l.prompts = !F32 && a.tiles && work > kLittle;
+        if (MASK && work <= kLittle) l.width = kNarrow;
         lds_barrier();
     }
     int length = 0, units = 0, longest = 0, rows = 0;          // (16 entries a thread at most: their rows are an int)
     for (int b = lo; b < hi; ++b) {
         const kv_entry e = kv_entry_of(a.v, a.rows, b);
-        const entry_span s = span_of<MASK>(a, e.len, e.rows);
+        const entry_span s = span_of<MASK>(a, e.len, e.rows, l.width);
         const bool here = s.n && !is_prompt(a, l, e.rows);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.who[b] = int2{e.slot, e.len};
@@ -214,7 +222,7 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     l.even = uniform(total_units <= (int)gridDim.x && longest <= kShort && a.grain == 0 ? longest : 0);
     for (int b = lo; b < hi; ++b) {
         const int4 e = l.entry(b);
-        const entry_span s = span_of<MASK>(a, e.y, e.w);
+        const entry_span s = span_of<MASK>(a, e.y, e.w, l.width);
         const bool here = s.n && !is_prompt(a, l, e.w);
         const int size = here ? ((s.n - 1) >> a.grain) + 1 + kUnitCost : 0, u = here ? s.groups * a.v.heads : 0;
         l.at[b] = l.even ? units_at * l.even : length_at;
@@ -324,48 +332,43 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : ~0u >> (32 - min(n, 32)); }
 struct column_sight {
-    int lo, hi;                // the window
-    int end;                   // no token from here on; 0: the column does not exist
-    int tree;                  // token of bit 0 of the line
-    const uint32_t* line;
-    bool any;                  // it sees a token
-    // pos: of its row; j: the row's number of the entry's `rows`; row: of all rows
-    __device__ __forceinline__ column_sight(const attn_args& a, int len, int rows, int j, int row, bool real) {
+    int lo, hi;                // of the window; hi: 0 where the column does not exist
+    int line;                  // its row's words begin here; below 0: it has none
+    // pos: of its row; j: the row's number of the entry's `rows`; row: of all rows; any: whether it sees a token
+    __device__ __forceinline__ column_sight(const attn_args& a, int len, int rows, int j, int row, bool real, bool& any) {
         const int base = len - rows;
         int pos = base + j;
         hi = min(pos + 1, len);
-        end = hi;
-        tree = base;
-        line = nullptr;
+        line = -1;
         any = false;
         if (a.line_words) {
-            line = a.lines + (size_t)row * a.line_words;
+            line = row * a.line_words;                         // 2^24 rows of 32 words are below 2^31
             // the row's depth: the others of its entry that it sees
             const int words = min(a.line_words, (rows + 31) / 32);
             pos = base;
             for (int w = 0; w < words; ++w) {
-                const uint32_t seen = line[w] & bits_below(rows - 32 * w) & ~bits_below(-base - 32 * w);
+                const uint32_t seen = a.lines[line + w] & bits_below(rows - 32 * w) & ~bits_below(-base - 32 * w);
                 any |= seen != 0;
                 pos += __popc(j >> 5 == w ? seen & ~(1u << (j & 31)) : seen);
             }
             hi = base;
-            end = len;
         }
         lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
-        any |= lo < hi || min(a.sinks, hi) > 0;
+        any = real && (any || lo < hi || min(a.sinks, hi) > 0);
         if (!real) {
-            any = false;
-            end = 0;
+            hi = 0;
+            line = -1;
         }
     }
-    __device__ __forceinline__ uint32_t seen(const attn_args& a, int t0) const {
+    // bit i: it sees token t0 + i of the sequence
+    __device__ __forceinline__ uint32_t seen(const attn_args& a, int len, int rows, int t0) const {
         uint32_t bits = bits_below(hi - t0) & (~bits_below(lo - t0) | bits_below(a.sinks - t0));
-        if (a.line_words && t0 + 32 > tree) {
-            const int u = t0 - tree, w = u >> 5;
-            const uint32_t x = w >= 0 && w < a.line_words ? line[w] : 0u, y = w + 1 < a.line_words ? line[w + 1] : 0u;
-            bits |= __builtin_amdgcn_alignbit(y, x, (unsigned)u & 31u);
+        const int u = t0 - (len - rows), w = u >> 5;           // the row of token t0, of the tree
+        if (a.line_words && u > -32 && line >= 0) {
+            const uint32_t x = w >= 0 && w < a.line_words ? a.lines[line + w] : 0u, y = w + 1 < a.line_words ? a.lines[line + w + 1] : 0u;
+            bits |= __builtin_amdgcn_alignbit(y, x, (unsigned)u & 31u) & bits_below(len - t0);
         }
-        return bits & bits_below(end - t0);
+        return bits;
     }
 };
 
@@ -380,29 +383,49 @@ __device__ __forceinline__ part_range parts_of(int unit_at, int size, int part) 
     return {divide(unit_at + SNAP - 1, part), divide(unit_at + size - SNAP, part)};
 }
 
-// Parts of units that other workgroups read: written through to where every XCD sees them, and read from there, eight bytes
-// at a time (slot: the workgroup's part of the unit that began before it, or of the one that goes on after it).
-template <int D, int COLUMNS>
+// Parts of units that other workgroups read: written through to where every XCD sees them, and read from there (slot: the
+// workgroup's part of the unit that began before it, or of the one that goes on after it).  Eight bytes at a time, or sixteen (WIDE: buffer accesses,
+// sc1 of the cache policy: coherent over the device).  The stream kernel's parts are small and sixteen cost it a little (one sequence through a window of
+// 4096 14.5 -> 15.2 us); the prompt kernel's are not.
+constexpr int kDeviceCoherent = 16;
+template <int D, int COLUMNS, bool WIDE>
 __device__ __forceinline__ void put_part(float* parts, long long slot, int column, int c, const f32x4& y, float weight, float best) {
-    unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
     typedef __attribute__((ext_vector_type(2))) float f32x2;
+    if constexpr (WIDE) {
+        const rsrc_t part = make_rsrc(parts + (size_t)slot * COLUMNS * (D + 4));
+        const int at = column * (D + 4) * 4;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), part, at + 16 + 4 * c, 0, kDeviceCoherent);
+        typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+        if (c == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(weight), __float_as_uint(best)}, part, at, 0, kDeviceCoherent);
+    } else {
+        unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        __hip_atomic_store(p + 2 + c / 2 + i, __builtin_bit_cast(unsigned long long, f32x2{y[2 * i], y[2 * i + 1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (c == 0) __hip_atomic_store(p, __builtin_bit_cast(unsigned long long, f32x2{weight, best}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int i = 0; i < 2; ++i)
+            __hip_atomic_store(p + 2 + c / 2 + i, __builtin_bit_cast(unsigned long long, f32x2{y[2 * i], y[2 * i + 1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (c == 0) __hip_atomic_store(p, __builtin_bit_cast(unsigned long long, f32x2{weight, best}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
 }
-template <int D, int COLUMNS>
+template <int D, int COLUMNS, bool WIDE>
 __device__ __forceinline__ void get_part(const float* parts, long long slot, int column, int c, f32x4& y, float& weight, float& best) {
-    const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
     typedef __attribute__((ext_vector_type(2))) float f32x2;
-    const f32x2 head = __builtin_bit_cast(f32x2, __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-    weight = head[0];
-    best = head[1];
+    if constexpr (WIDE) {
+        const rsrc_t part = make_rsrc(parts + (size_t)slot * COLUMNS * (D + 4));
+        const int at = column * (D + 4) * 4;
+        y = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at + 16 + 4 * c, 0, kDeviceCoherent));
+        const auto head = __builtin_amdgcn_raw_buffer_load_b64(part, at, 0, kDeviceCoherent);
+        weight = __uint_as_float(head[0]);
+        best = __uint_as_float(head[1]);
+    } else {
+        const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
+        const f32x2 head = __builtin_bit_cast(f32x2, __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        weight = head[0];
+        best = head[1];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const f32x2 x = __builtin_bit_cast(f32x2, __hip_atomic_load(p + 2 + c / 2 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        y[2 * i] = x[0];
-        y[2 * i + 1] = x[1];
+        for (int i = 0; i < 2; ++i) {
+            const f32x2 x = __builtin_bit_cast(f32x2, __hip_atomic_load(p + 2 + c / 2 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            y[2 * i] = x[0];
+            y[2 * i + 1] = x[1];
+        }
     }
 }
 // Whether this workgroup is the last of others + 1 to come here; it leaves the count at 0.  Parts were written through: once
@@ -422,36 +445,63 @@ __device__ __forceinline__ bool last_to_come(int* count, int others, int* last_o
 // Parts w_first .. w_last of a unit, this workgroup's among them and written, become its result: in two steps, sixteen
 // consecutive ones and then the sixteens, so that a workgroup reads at most 16 + 64 of them.  A column's quads are neighbouring
 // lanes: all of them have read a part before one writes the sixteen's sum in its place.
-template <int D, int COLUMNS, int THREADS, class Finish>
+template <int D, int COLUMNS, int THREADS, bool WIDE, bool MASK, class Finish>
 __device__ void join_parts(float* parts, int* done, int w_first, int w_last, int columns, int* last_one, Finish finish) {
     constexpr int QUADS = D / 4;
     const int group = ((int)blockIdx.x - w_first) >> 4, g_first = w_first + 16 * group, g_last = min(g_first + 15, w_last), groups = (w_last - w_first >> 4) + 1;
-    const auto join = [&](int from, int to, int step, bool final) {
-        for (int i = threadIdx.x; i < columns * QUADS; i += THREADS) {
-            const int col = i / QUADS, c = 4 * (i % QUADS);
-            float best = -kFar, weight = 0.f;
-            f32x4 y = {0.f, 0.f, 0.f, 0.f};
-            for (int w = from; w <= to; w += 8 * step) {
-                f32x4 in[8];
-                float in_weight[8], in_best[8];
+    // AT_ONCE of a thread's quads, PARTS parts on their way together: what a join takes is the way to the parts and back
+    const auto join_some = [&](auto at_once, auto some_parts, int from, int to, int step, bool final) {
+        constexpr int AT_ONCE = decltype(at_once)::value, PARTS = decltype(some_parts)::value;
+        for (int i0 = threadIdx.x; i0 < columns * QUADS; i0 += AT_ONCE * THREADS) {
+            int col[AT_ONCE], c[AT_ONCE];
+            float best[AT_ONCE], weight[AT_ONCE];
+            f32x4 y[AT_ONCE];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int ww = min(w + k * step, to);                      // those past the end are read twice and not used
-                    get_part<D, COLUMNS>(parts, 2 * (long long)ww + (ww == w_first), col, c, in[k], in_weight[k], in_best[k]);
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = AT_ONCE == 1 ? i0 : min(i0 + u * THREADS, columns * QUADS - 1);          // those past the end are not used
+                col[u] = i / QUADS;
+                c[u] = 4 * (i % QUADS);
+                best[u] = -kFar;
+                weight[u] = 0.f;
+                y[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            for (int w = from; w <= to; w += PARTS * step) {
+                f32x4 in[AT_ONCE][PARTS];
+                float in_weight[AT_ONCE][PARTS], in_best[AT_ONCE][PARTS];
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {
+                    if (MASK && w + k * step > to) break;
+                    const int ww = min(w + k * step, to);                      // (those past the end are read twice and not used)
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u)
+                        get_part<D, COLUMNS, WIDE>(parts, 2 * (long long)ww + (ww == w_first), col[u], c[u], in[u][k], in_weight[u][k], in_best[u][k]);
                 }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < PARTS; ++k)
                     if (w + k * step <= to) {
-                        const float now = fmaxf(best, in_best[k]);
-                        const float f = best == now ? 1.f : __builtin_amdgcn_exp2f(best - now), f2 = in_best[k] == now ? 1.f : __builtin_amdgcn_exp2f(in_best[k] - now);
-                        y = y * f + in[k] * f2;
-                        weight = weight * f + in_weight[k] * f2;
-                        best = now;
+#pragma unroll
+                        for (int u = 0; u < AT_ONCE; ++u) {
+                            const float now = fmaxf(best[u], in_best[u][k]);
+                            const float f = best[u] == now ? 1.f : __builtin_amdgcn_exp2f(best[u] - now), f2 = in_best[u][k] == now ? 1.f : __builtin_amdgcn_exp2f(in_best[u][k] - now);
+                            y[u] = y[u] * f + in[u][k] * f2;
+                            weight[u] = weight[u] * f + in_weight[u][k] * f2;
+                            best[u] = now;
+                        }
                     }
             }
-            if (final) finish(col, c, y, weight);
-            else put_part<D, COLUMNS>(parts, 2 * (long long)from + (from == w_first), col, c, y, weight, best);
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (AT_ONCE == 1 || i0 + u * THREADS < columns * QUADS) {
+                    if (final) finish(col[u], c[u], y[u], weight[u]);
+                    else put_part<D, COLUMNS, WIDE>(parts, 2 * (long long)from + (from == w_first), col[u], c[u], y[u], weight[u], best[u]);
+                }
         }
+    };
+    const auto join = [&](int from, int to, int step, bool final) {
+        using std::integral_constant;
+        if (WIDE && (to - from) / step < 2 && columns * QUADS > 2 * THREADS) join_some(integral_constant<int, 4>(), integral_constant<int, 2>(), from, to, step, final);
+        else if (MASK && (to - from) / step < 4 && columns * QUADS > THREADS) join_some(integral_constant<int, 2>(), integral_constant<int, 4>(), from, to, step, final);
+        else join_some(integral_constant<int, 1>(), integral_constant<int, 8>(), from, to, step, final);
     };
     if (g_last > g_first) {
         if (!last_to_come(&done[2 * g_first], g_last - g_first, last_one)) return;
@@ -872,7 +922,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         const int4 e = list.entry(b);
         place p;
         p.entry = int4{uniform(e.x), uniform(e.y), uniform(e.z), uniform(e.w)};
-        p.sp = span_of<MASK>(a, p.entry.y, p.entry.w);
+        p.sp = span_of<MASK>(a, p.entry.y, p.entry.w, MASK ? list.width : kColumns);
         p.grains = ((p.sp.n - 1) >> a.grain) + 1;
         p.size = list.even ? list.even : p.grains + kUnitCost;
         const int in = uniform(at - list.at[b]);
@@ -899,8 +949,8 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         if (to <= from) continue;
         const int first = from << a.grain, stop = min(to << a.grain, sp.n);
         const bool begins = from == 0, complete = begins && to == grains;
-        const int head = sp.groups == 1 ? unit : divide(unit, sp.groups), column0 = (unit - head * sp.groups) * kColumns;
-        const int columns = min(rows * a.g - column0, kColumns);
+        const int head = sp.groups == 1 ? unit : divide(unit, sp.groups), width = MASK ? uniform(list.width) : kColumns, column0 = (unit - head * sp.groups) * width;
+        const int columns = min(rows * a.g - column0, width);
         const int tiles = columns > 32 ? 4 : columns > 16 ? 2 : 1, stripes = 4 / tiles, tile = wave & (tiles - 1), stripe = wave / tiles;
         const int j0 = divide(column0, a.g), r0 = column0 - j0 * a.g;      // a column's row and head: those of r0 + column in rows of g, from row j0 on
         // what the wave's columns see: any of them, all of them
@@ -960,10 +1010,11 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 #pragma unroll
             for (int i = 0; i < KK; ++i) load_raw(a.Q, from + 32 * i, q[i]);
         }
+        bool sees_any;
+        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real, sees_any);
         // waited for here: loads into LDS that the compiler does not know of would be waited for with them
         asm volatile("" : "+v"(pages));
         if (MASK) asm volatile("" : "+v"(next_pages));
-        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real);
 #pragma unroll
         for (int i = 0; i < KK; ++i)
 #pragma unroll
@@ -973,13 +1024,13 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         for (int i = 0; i < S; ++i)
             if (k + i * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + i * stripes), lane);
         attn_state<D, F32, MASK> st;
-        st.start(a, q, len, len - rows + j0 + j, real, MASK && sight.any);
+        st.start(a, q, len, len - rows + j0 + j, real, sees_any);
         for (int i = 0; k < b1; k += stripes) {
             if (k + (S - 1) * stripes < b1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kBlockLoads<D>) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             const int t0 = block_of(k) * kKvBlock;
             st.step(ring + (wave * S + i) * BLOCK, t0, (t0 >= all_lo || (MASK && t0 + kKvBlock <= a.sinks)) && t0 + kKvBlock <= all_hi, lane,
-                    [&] { if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane); }, [&] { return sight.seen(a, t0); });
+                    [&] { if (k + S * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + S * stripes), lane); }, [&] { return sight.seen(a, len, rows, t0); });
             i = i + 1 == S ? 0 : i + 1;
         }
         // the four quarters of a column's tokens, then the waves that share columns
@@ -987,6 +1038,12 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 #pragma unroll
         for (int gr = 0; gr < D / kKvGroup; ++gr) st.mid[gr] = quarters_sum(st.mid[gr]);
         const float top2 = st.top > -kFar ? st.top * st.kappa : -kFar;         // as an exponent of 2
+        // Y of four channels of a column from its weighted values and the weights' sum
+        const auto finish = [&](int col, int c, const f32x4& y, float weight) {
+            const int x = r0 + col, j = over_g(x);
+            put_out(a.Y, (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + x - j * a.g) * D + c,
+                    weight == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * __builtin_amdgcn_rcpf(weight));
+        };
         lds_barrier();                                         // all blocks have been read
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) *(f32x4*)&merged[wave][lane & 15][16 * i + 4 * h] = st.o[i] * st.scale_unlift(i / 4) + st.mid[i / 4];
@@ -995,12 +1052,6 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
             wtop[wave][lane] = top2;
         }
         lds_barrier();
-        // Y of four channels of a column from its weighted values and the weights' sum
-        const auto finish = [&](int col, int c, const f32x4& y, float weight) {
-            const int x = r0 + col, j = over_g(x);
-            put_out(a.Y, (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + x - j * a.g) * D + c,
-                    weight == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * __builtin_amdgcn_rcpf(weight));
-        };
         for (int i = threadIdx.x; i < columns * QUADS; i += 256) {
             const int col = i / QUADS, c = 4 * (i % QUADS), w0 = col >> 4, l = col & 15;
             float best = -kFar, weight = 0.f;
@@ -1015,11 +1066,11 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
                     weight += f * wsum[w][l];
                 }
             if (complete) finish(col, c, y, weight);
-            else put_part<D, kColumns>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
+            else put_part<D, kColumns, false>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
         }
         if (complete) continue;
         const part_range parts = parts_of<kSnap>(unit_at, size, part);
-        join_parts<D, kColumns, 256>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
+        join_parts<D, kColumns, 256, false, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
     // rows that see nothing: no unit holds them
     const int width = a.g * a.v.heads * QUADS;
@@ -1174,8 +1225,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 all_hi = len - rows;
             }
         }
-        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real);
-        const bool sees_any = MASK ? sight.any : vlo < vhi;
+        bool masked_any;
+        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real, masked_any);
+        const bool sees_any = MASK ? masked_any : vlo < vhi;
         // a thread's words of a stage (its block of the two; past the end the last one's again)
         const int* table = a.v.table + (size_t)max(slot, 0) * a.v.max_pages;
         const int last_block = max((len + kKvBlock - 1) / kKvBlock - 1, 0);
@@ -1368,7 +1420,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                     if (MASK && !whole) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const uint32_t bits = sight.seen(a, t0 + 32 * i) >> (4 * hh);
+                            const uint32_t bits = sight.seen(a, len, rows, t0 + 32 * i) >> (4 * hh);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) s[i][k] = bits >> ((k & 3) + 8 * (k >> 2)) & 1u ? s[i][k] : -INFINITY;
                         }
@@ -1414,7 +1466,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                             bool sees = false;
 #pragma unroll 1
                             for (int t = 0; t < (MASK ? 0 : kStage); ++t) sees |= (nans[stage & 3][2 * gr + (t >> 5)] >> (t & 31) & 1) && t0 + t >= vlo && t0 + t < vhi;
-                            if (MASK) sees = (nans[stage & 3][2 * gr] & sight.seen(a, t0)) | (nans[stage & 3][2 * gr + 1] & sight.seen(a, t0 + 32));
+                            if (MASK) sees = (nans[stage & 3][2 * gr] & sight.seen(a, len, rows, t0)) | (nans[stage & 3][2 * gr + 1] & sight.seen(a, len, rows, t0 + 32));
                             if (sees)
 #pragma unroll
                                 for (int ot = 0; ot < 2; ++ot)
@@ -1491,12 +1543,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             for (int ot = 0; ot < OT; ++ot)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    put_part<D, kTile>(a.parts, 2 * (long long)blockIdx.x + begins, column, 32 * ot + 8 * k + 4 * hh,
+                    put_part<D, kTile, MASK>(a.parts, 2 * (long long)blockIdx.x + begins, column, 32 * ot + 8 * k + 4 * hh,
                                        f32x4{o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]}, sum, best);
         }
         if (complete) continue;
         const part_range parts = parts_of<kTileSnap>(unit_at, size, part);
-        join_parts<D, kTile, kTileThreads>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
+        join_parts<D, kTile, kTileThreads, MASK, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
 }
 
