@@ -331,30 +331,40 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
 // Masks: what a column sees, 32 tokens at a time.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : ~0u >> (32 - min(n, 32)); }
+// AHEAD: the row's first two words are asked for when the column begins (trees of up to 64 rows have no more).
+template <bool AHEAD>
 struct column_sight {
     int lo, hi;                // of the window; hi: 0 where the column does not exist
     int line;                  // its row's words begin here; below 0: it has none
-    // pos: of its row; j: the row's number of the entry's `rows`; row: of all rows; any: whether it sees a token
-    __device__ __forceinline__ column_sight(const attn_args& a, int len, int rows, int j, int row, bool real, bool& any) {
+    uint32_t first[AHEAD ? 2 : 1];
+    __device__ __forceinline__ uint32_t word(const attn_args& a, int w) const {
+        if (w < 0 || w >= a.line_words) return 0u;
+        return AHEAD && w < 2 ? w ? first[AHEAD] : first[0] : a.lines[line + w];
+    }
+    // pos: of its row; j: the row's number of the entry's `rows`; row: of all rows
+    __device__ __forceinline__ column_sight(const attn_args& a, int len, int rows, int j, int row, bool real) {
         const int base = len - rows;
         int pos = base + j;
         hi = min(pos + 1, len);
         line = -1;
-        any = false;
         if (a.line_words) {
             line = row * a.line_words;                         // 2^24 rows of 32 words are below 2^31
-            // the row's depth: the others of its entry that it sees
-            const int words = min(a.line_words, (rows + 31) / 32);
-            pos = base;
-            for (int w = 0; w < words; ++w) {
-                const uint32_t seen = a.lines[line + w] & bits_below(rows - 32 * w) & ~bits_below(-base - 32 * w);
-                any |= seen != 0;
-                pos += __popc(j >> 5 == w ? seen & ~(1u << (j & 31)) : seen);
+            if constexpr (AHEAD) {
+                const uint2 w = *(const uint2*)(a.lines + line);               // words of 64 bits
+                first[0] = w.x;
+                first[1] = w.y;
+            }
+            if (a.window > 0) {                                // the row's depth: the others of its entry that it sees
+                const int words = min(a.line_words, (rows + 31) / 32);
+                pos = base;
+                for (int w = 0; w < words; ++w) {
+                    const uint32_t seen = word(a, w) & bits_below(rows - 32 * w) & ~bits_below(-base - 32 * w);
+                    pos += __popc(j >> 5 == w ? seen & ~(1u << (j & 31)) : seen);
+                }
             }
             hi = base;
         }
         lo = a.window > 0 ? max(pos - a.window + 1, 0) : 0;
-        any = real && (any || lo < hi || min(a.sinks, hi) > 0);
         if (!real) {
             hi = 0;
             line = -1;
@@ -363,12 +373,16 @@ struct column_sight {
     // bit i: it sees token t0 + i of the sequence
     __device__ __forceinline__ uint32_t seen(const attn_args& a, int len, int rows, int t0) const {
         uint32_t bits = bits_below(hi - t0) & (~bits_below(lo - t0) | bits_below(a.sinks - t0));
-        const int u = t0 - (len - rows), w = u >> 5;           // the row of token t0, of the tree
-        if (a.line_words && u > -32 && line >= 0) {
-            const uint32_t x = w >= 0 && w < a.line_words ? a.lines[line + w] : 0u, y = w + 1 < a.line_words ? a.lines[line + w + 1] : 0u;
-            bits |= __builtin_amdgcn_alignbit(y, x, (unsigned)u & 31u) & bits_below(len - t0);
-        }
+        const int u = t0 - (len - rows);                       // the row of token t0, of the tree
+        if (a.line_words && u > -32 && line >= 0) bits |= __builtin_amdgcn_alignbit(word(a, (u >> 5) + 1), word(a, u >> 5), (unsigned)u & 31u) & bits_below(len - t0);
         return bits;
+    }
+    // whether it sees a token at all (rarely asked)
+    __device__ bool any(const attn_args& a, int len, int rows) const {
+        bool some = lo < hi || min(a.sinks, hi) > 0;
+        if (line >= 0)
+            for (int w = 0; w < min(a.line_words, (rows + 31) / 32); ++w) some |= (word(a, w) & bits_below(rows - 32 * w) & ~bits_below(rows - len - 32 * w)) != 0;
+        return some;
     }
 };
 
@@ -634,7 +648,8 @@ struct attn_state {
 
     // w: the lane's channels 32 k + 8 (lane / 16) .. + 7 as they are in memory; pos: position of the column's row; real: the column exists
     static constexpr int RAW = F32 ? 8 : 4;                    // words of 8 channels
-    __device__ __forceinline__ void start(const attn_args& a, uint32_t (&w)[KK][RAW], int len, int pos, bool real, bool sees) {
+    template <class Sees>
+    __device__ __forceinline__ void start(const attn_args& a, uint32_t (&w)[KK][RAW], int len, int pos, bool real, Sees sees) {
         // a negative scale is the queries' sign
         const uint32_t sign = a.scale < 0.f ? (F32 ? 0x80000000u : 0x80008000u) : 0u;
         bool finite;
@@ -687,7 +702,7 @@ struct attn_state {
         vlo = real ? (a.window > 0 ? max(pos - a.window + 1, 0) : 0) : 0;
         top = -kFar;
         down = kLift;
-        sum = real && !finite && (MASK ? sees : vlo < vhi) ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
+        sum = real && !finite && (MASK ? sees() : vlo < vhi) ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
             mid[gr] = 0.f;
@@ -1010,8 +1025,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
 #pragma unroll
             for (int i = 0; i < KK; ++i) load_raw(a.Q, from + 32 * i, q[i]);
         }
-        bool sees_any;
-        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real, sees_any);
+        const column_sight<true> sight(a, len, rows, j0 + j, row0 + j0 + j, real);
         // waited for here: loads into LDS that the compiler does not know of would be waited for with them
         asm volatile("" : "+v"(pages));
         if (MASK) asm volatile("" : "+v"(next_pages));
@@ -1024,7 +1038,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
         for (int i = 0; i < S; ++i)
             if (k + i * stripes < b1) fetch_block<D>(my_ring + i * BLOCK, block_at(k + i * stripes), lane);
         attn_state<D, F32, MASK> st;
-        st.start(a, q, len, len - rows + j0 + j, real, sees_any);
+        st.start(a, q, len, len - rows + j0 + j, real, [&] { return sight.any(a, len, rows); });
         for (int i = 0; k < b1; k += stripes) {
             if (k + (S - 1) * stripes < b1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((S - 1) * kBlockLoads<D>) : "memory");
             else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -1225,9 +1239,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 all_hi = len - rows;
             }
         }
-        bool masked_any;
-        const column_sight sight(a, len, rows, j0 + j, row0 + j0 + j, real, masked_any);
-        const bool sees_any = MASK ? masked_any : vlo < vhi;
+        const column_sight<false> sight(a, len, rows, j0 + j, row0 + j0 + j, real);
         // a thread's words of a stage (its block of the two; past the end the last one's again)
         const int* table = a.v.table + (size_t)max(slot, 0) * a.v.max_pages;
         const int last_block = max((len + kKvBlock - 1) / kKvBlock - 1, 0);
@@ -1371,7 +1383,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                     q[k][2 * i] = (_Float16)(__uint_as_float(y << 16) * f);
                     q[k][2 * i + 1] = (_Float16)(__uint_as_float(y & 0xffff0000u) * f);
                 }
-            sum = real && !finite && sees_any ? NAN : 0.f;
+            sum = real && !finite && (MASK ? sight.any(a, len, rows) : vlo < vhi) ? NAN : 0.f;
         }
         const float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
         float top = -kFar, down = kTileLift;

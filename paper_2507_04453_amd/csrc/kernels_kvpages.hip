@@ -83,11 +83,12 @@ __device__ int entry_sums(int* prefix, int n, int* waves) {
     return total;
 }
 
-__global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len, int max_seqs, int32_t* refs, int n_pages, int32_t* done) {
+__global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len, int max_seqs, int32_t* refs, int n_pages, int32_t* done, int32_t* come) {
     const long long step = (long long)gridDim.x * blockDim.x;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < entries; i += step) table[i] = -1;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < max_seqs; i += step) len[i] = 0;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < 2 * essa_k::kKvAttnWorkgroups; i += step) done[i] = 0;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < max_seqs; i += step) come[i] = 0;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_pages; i += step) refs[i] = 0;
 }
 
@@ -265,14 +266,14 @@ __global__ __launch_bounds__(256) void kv_fork_tables_kernel(pages_view v, const
 // Keeping a path of a tree's rows.  Entry b's rows are its sequence's last ones; rows path[0] < path[1] < .. of them stay, row path[i] as token base + i,
 // so that a token only ever moves towards the front: with the blocks that tokens move into done in order, each read whole before it is written, no
 // token is overwritten before it has moved.  Workgroup (b, y) looks for itself whether the entry can be served and moves its share of the heads of
-// all layers; (b, 0) leaves the answer for the launch that gives pages back.
+// all layers; the last of an entry's to have done so, when nobody looks at its tables any more, gives the pages behind the path back.
 struct accept_entry {
     int ok;                    // the sequence, or why not
-    int row0, base, keep, moved;   // moved: the first row of the path that is not where it was
+    int row0, len, base, keep, moved;   // moved: the first row of the path that is not where it was
 };
 __device__ accept_entry accept_of(const pages_view& v, const essa_k::kv_rows& rows, const int32_t* path, const int32_t* keep, int b) {     // 256 threads
     __shared__ int moved;
-    accept_entry e{rows.seqs[b], b, 0, keep[b], 0};
+    accept_entry e{rows.seqs[b], b, 0, 0, keep[b], 0};
     int c = 1;
     if (rows.row_start) {
         e.row0 = min(max(rows.row_start[b], 0), rows.R);
@@ -285,6 +286,7 @@ __device__ accept_entry accept_of(const pages_view& v, const essa_k::kv_rows& ro
     if (threadIdx.x == 0) moved = e.keep;
     bool bad = e.ok >= v.max_seqs;
     const int len = bad ? 0 : v.length(e.ok);
+    e.len = len;
     e.base = len - c;
     bad |= e.keep < 0 || e.keep > c || e.base < 0;
     for (int j = threadIdx.x; j < b; j += 256) bad |= rows.seqs[j] == e.ok;
@@ -307,20 +309,20 @@ __device__ accept_entry accept_of(const pages_view& v, const essa_k::kv_rows& ro
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void kv_accept_move_kernel(pages_view v, essa_k::kv_rows rows, const int32_t* path, const int32_t* keep, unsigned char* pool,
-                                                             long long page_bytes, int head_bytes, int heads) {
+__global__ __launch_bounds__(256) void kv_accept_kernel(pages_view v, essa_k::kv_rows rows, const int32_t* path, const int32_t* keep, int32_t* served, unsigned char* pool,
+                                                        long long page_bytes, int head_bytes, int heads) {
     constexpr int NG = D / kKvGroup, KW = D / 64, VECS = D / 32;               // of a thread: words of keys, vectors of values
     __shared__ unsigned char codes[kKvBlock][D + 4];
     const int b = blockIdx.x;
     const accept_entry e = accept_of(v, rows, path, keep, b);
-    if (blockIdx.y == 0 && threadIdx.x == 0) v.s.entry_ok[b] = e.ok;
-    if (e.ok < 0 || e.moved >= e.keep) return;
+    if (served && blockIdx.y == 0 && threadIdx.x == 0) served[b] = e.ok;
+    const bool moves = e.ok >= 0 && e.moved < e.keep;
     const int tok = threadIdx.x / 8, part = threadIdx.x % 8, per_page = v.page_tokens / kKvBlock;
     const auto block_at = [&](int head, int block) {
         return pool + v.page(e.ok, block / per_page) * page_bytes + (long long)head * head_bytes + (size_t)(block % per_page) * essa_k::kv_block_bytes(D);
     };
     const auto scale_at = [&](int side, int group, int t) { return (side ? essa_k::kv_value_scales_at(D) : essa_k::kv_key_scales_at(D)) + kv_scale_at(group, t); };
-    for (int head = blockIdx.y; head < heads; head += gridDim.y)
+    for (int head = blockIdx.y; moves && head < heads; head += gridDim.y)
         for (int block = (e.base + e.moved) / kKvBlock; block * kKvBlock < e.base + e.keep; ++block) {
             const int t0 = block * kKvBlock, first = max(e.base + e.moved - t0, 0), last = min(e.base + e.keep - t0, kKvBlock);
             unsigned char* out = block_at(head, block);
@@ -376,24 +378,23 @@ __global__ __launch_bounds__(256) void kv_accept_move_kernel(pages_view v, essa_
                 *to = (*to & keep_bits) | w;
             }
         }
-}
-
-__global__ __launch_bounds__(256) void kv_accept_tables_kernel(pages_view v, essa_k::kv_rows rows, const int32_t* keep, int32_t* served) {
-    const int b = blockIdx.x, ok = v.s.entry_ok[b];
-    if (threadIdx.x == 0 && served) served[b] = ok;
-    if (ok < 0) return;
-    int c = 1;
-    if (rows.row_start) {
-        const int row0 = min(max(rows.row_start[b], 0), rows.R);
-        c = min(max(rows.row_start[b + 1], row0), rows.R) - row0;
+    if (gridDim.y > 1) {                                       // every workgroup is counted, whatever it was told by tables that somebody spoiled
+        __shared__ bool last;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            last = atomicAdd(&v.s.come[b], 1) == (int)gridDim.y - 1;
+            if (last) v.s.come[b] = 0;
+        }
+        __syncthreads();
+        if (!last) return;
     }
-    const int len = v.length(ok), now = len - c + keep[b];
-    __syncthreads();                                           // everybody has the old length
-    for (int f = v.pages(now) + (int)threadIdx.x; f < v.pages(len); f += 256) {
-        atomicSub(&v.refs[v.page(ok, f)], 1);
-        v.table[(size_t)ok * v.max_pages + f] = -1;
+    if (e.ok < 0) return;
+    const int now = e.base + e.keep;
+    for (int f = v.pages(now) + (int)threadIdx.x; f < v.pages(e.len); f += 256) {
+        atomicSub(&v.refs[v.page(e.ok, f)], 1);
+        v.table[(size_t)e.ok * v.max_pages + f] = -1;
     }
-    if (threadIdx.x == 0) v.len[ok] = now;
+    if (threadIdx.x == 0) v.len[e.ok] = now;
 }
 
 // Compaction: count the pages in use, list those above and the holes below (ascending), and every page's new index.
@@ -473,7 +474,7 @@ pages_view view_of(const essa_kv* kv) {
 namespace essa_k {
 
 size_t kv_scratch_words(const essa_kv_desc& d) {
-    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4 + 2 * kKvAttnWorkgroups;
+    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4 + 2 * kKvAttnWorkgroups + d.max_seqs;
 }
 kv_scratch kv_scratch_of(const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
@@ -485,13 +486,14 @@ kv_scratch kv_scratch_of(const essa_kv* kv) {
     s.entry_ok = s.entry_page + d.max_seqs;
     s.count = s.entry_ok + d.max_seqs;
     s.done = s.count + 4;
-    s.rows = s.done + 2 * kKvAttnWorkgroups;
+    s.come = s.done + 2 * kKvAttnWorkgroups;
+    s.rows = s.come + d.max_seqs;
     return s;
 }
 
 hipError_t kv_clear(hipStream_t st, const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
-    kv_clear_kernel<<<512, 256, 0, st>>>(d.table, (long long)d.max_seqs * d.max_pages, d.len, d.max_seqs, d.refs, d.n_pages, kv_scratch_of(kv).done);
+    kv_clear_kernel<<<512, 256, 0, st>>>(d.table, (long long)d.max_seqs * d.max_pages, d.len, d.max_seqs, d.refs, d.n_pages, kv_scratch_of(kv).done, kv_scratch_of(kv).come);
     return hipGetLastError();
 }
 
@@ -518,9 +520,8 @@ hipError_t kv_accept(hipStream_t st, const essa_kv* kv, const kv_rows& rows, con
     const essa_kv_desc& d = kv->d;
     const pages_view v = view_of(kv);
     const int per_head = kv_block_bytes(d.head_dim) * (d.page_tokens / kKvBlock), heads = d.layers * d.n_kv_heads;
-    const auto move = d.head_dim == 64 ? kv_accept_move_kernel<64> : kv_accept_move_kernel<128>;
-    move<<<dim3(rows.n, std::min(heads, 64)), 256, 0, st>>>(v, rows, path, keep, (unsigned char*)d.pool, (long long)per_head * heads, per_head, heads);
-    kv_accept_tables_kernel<<<rows.n, 256, 0, st>>>(v, rows, keep, served);
+    (d.head_dim == 64 ? kv_accept_kernel<64> : kv_accept_kernel<128>)<<<dim3(rows.n, std::min(heads, 64)), 256, 0, st>>>(
+        v, rows, path, keep, served, (unsigned char*)d.pool, (long long)per_head * heads, per_head, heads);
     return hipGetLastError();
 }
 
