@@ -90,7 +90,11 @@ struct attn_args {
 };
 // kTileCost and kTileSnap, in stages: 8192 rows take 714 us with a cost of 1, 584 with 3, 581 with 6; 16 prompts of 1024 rows 254, 237, 246; 32
 // times 300 rows behind 200 tokens 162 us with kTileSnap = 5, 116 with 8, 114 with 14 (16 of 1024: 251, 237, 216).
-constexpr int kTile = 256, kStage = 64, kTileCost = 3, kTileSnap = 8;
+// With masks, whose parts are joined faster: 48 trees of 26 rows (28 heads on 4) behind 104 to 3974 tokens 61 us with 3 and 8, 57 with 3 and 5, 58 with 4 and 5, 62 with 4 and 6, 12 prompts of
+// 90 to 6000 rows through a window of 1000 (40 on 8) 325, 328, 306, 307.
+constexpr int kTile = 256, kStage = 64;
+template <bool MASK> constexpr int kTileCost = MASK ? 4 : 3;
+template <bool MASK> constexpr int kTileSnap = MASK ? 5 : 8;
 // An entry whose rows fill more columns than a stream workgroup takes at once goes to the prompt kernel (bf16), where a block
 // is unpacked once for 256 columns instead of once for 16 -- unless all of the call is little work for the stream kernel
 // (kLittle, as its row of units would be long): tiles of 256 columns are then too few to fill the chip, or their parts too large to
@@ -316,7 +320,7 @@ __device__ void plan_tiles(const attn_args& a, const attn_list& l) {           /
             }
             const int4 e = l.entry(b);
             const tile_span t = tile_of<MASK>(a, e.y, e.w, i - first[b]);
-            size = ((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost;
+            size = ((t.n + (1 << a.tile_grain) - 1) >> a.tile_grain) + kTileCost<MASK>;
             a.tile[2 * i] = e;
             a.tile[2 * i + 1] = int4{i - first[b], t.lo, t.n, size};
         }
@@ -397,50 +401,50 @@ __device__ __forceinline__ part_range parts_of(int unit_at, int size, int part) 
     return {divide(unit_at + SNAP - 1, part), divide(unit_at + size - SNAP, part)};
 }
 
-// Parts of units that other workgroups read: written through to where every XCD sees them, and read from there (slot: the
-// workgroup's part of the unit that began before it, or of the one that goes on after it).  Eight bytes at a time, or sixteen (WIDE: buffer accesses,
-// sc1 of the cache policy: coherent over the device).  The stream kernel's parts are small and sixteen cost it a little (one sequence through a window of
-// 4096 14.5 -> 15.2 us); the prompt kernel's are not.
-constexpr int kDeviceCoherent = 16;
-template <int D, int COLUMNS, bool WIDE>
+// Parts of units that other workgroups read: written through to where every XCD sees them, and read from there, eight bytes
+// at a time (slot: the workgroup's part of the unit that began before it, or of the one that goes on after it).
+template <int D, int COLUMNS>
 __device__ __forceinline__ void put_part(float* parts, long long slot, int column, int c, const f32x4& y, float weight, float best) {
+    unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
     typedef __attribute__((ext_vector_type(2))) float f32x2;
-    if constexpr (WIDE) {
-        const rsrc_t part = make_rsrc(parts + (size_t)slot * COLUMNS * (D + 4));
-        const int at = column * (D + 4) * 4;
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y), part, at + 16 + 4 * c, 0, kDeviceCoherent);
-        typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
-        if (c == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(weight), __float_as_uint(best)}, part, at, 0, kDeviceCoherent);
-    } else {
-        unsigned long long* p = (unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            __hip_atomic_store(p + 2 + c / 2 + i, __builtin_bit_cast(unsigned long long, f32x2{y[2 * i], y[2 * i + 1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (c == 0) __hip_atomic_store(p, __builtin_bit_cast(unsigned long long, f32x2{weight, best}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = 0; i < 2; ++i)
+        __hip_atomic_store(p + 2 + c / 2 + i, __builtin_bit_cast(unsigned long long, f32x2{y[2 * i], y[2 * i + 1]}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (c == 0) __hip_atomic_store(p, __builtin_bit_cast(unsigned long long, f32x2{weight, best}), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <int D, int COLUMNS>
+__device__ __forceinline__ void get_part(const float* parts, long long slot, int column, int c, f32x4& y, float& weight, float& best) {
+    const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    const f32x2 head = __builtin_bit_cast(f32x2, __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+    weight = head[0];
+    best = head[1];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 x = __builtin_bit_cast(f32x2, __hip_atomic_load(p + 2 + c / 2 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+        y[2 * i] = x[0];
+        y[2 * i + 1] = x[1];
     }
 }
-template <int D, int COLUMNS, bool WIDE>
-__device__ __forceinline__ void get_part(const float* parts, long long slot, int column, int c, f32x4& y, float& weight, float& best) {
-    typedef __attribute__((ext_vector_type(2))) float f32x2;
-    if constexpr (WIDE) {
-        const rsrc_t part = make_rsrc(parts + (size_t)slot * COLUMNS * (D + 4));
-        const int at = column * (D + 4) * 4;
-        y = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, at + 16 + 4 * c, 0, kDeviceCoherent));
-        const auto head = __builtin_amdgcn_raw_buffer_load_b64(part, at, 0, kDeviceCoherent);
-        weight = __uint_as_float(head[0]);
-        best = __uint_as_float(head[1]);
-    } else {
-        const unsigned long long* p = (const unsigned long long*)(parts + ((size_t)slot * COLUMNS + column) * (D + 4));
-        const f32x2 head = __builtin_bit_cast(f32x2, __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-        weight = head[0];
-        best = head[1];
+// Parts of a tile as the prompt kernel's lanes hold them (masks): N quads of every thread, sixteen bytes at a time, a wave's next to one another, then every
+// column's sum and exponent.  Buffer accesses, sc1 of the cache policy: coherent over the device, as the others are.
+constexpr int kDeviceCoherent = 16;
+template <int D, int N>
+__device__ __forceinline__ void put_tile(float* parts, long long slot, const f32x4 (&y)[N], float weight, float best, bool heads, int column) {
+    const rsrc_t part = make_rsrc(parts + (size_t)slot * kTile * (D + 4));
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const f32x2 x = __builtin_bit_cast(f32x2, __hip_atomic_load(p + 2 + c / 2 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-            y[2 * i] = x[0];
-            y[2 * i + 1] = x[1];
-        }
-    }
+    for (int i = 0; i < N; ++i) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, y[i]), part, 16 * (512 * i + (int)threadIdx.x), 0, kDeviceCoherent);
+    typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+    if (heads) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(weight), __float_as_uint(best)}, part, 4 * kTile * D + 8 * column, 0, kDeviceCoherent);
+}
+template <int D, int N>
+__device__ __forceinline__ void get_tile(const float* parts, long long slot, f32x4 (&y)[N], float& weight, float& best, int column) {
+    const rsrc_t part = make_rsrc(parts + (size_t)slot * kTile * (D + 4));
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part, 16 * (512 * i + (int)threadIdx.x), 0, kDeviceCoherent));
+    const auto head = __builtin_amdgcn_raw_buffer_load_b64(part, 4 * kTile * D + 8 * column, 0, kDeviceCoherent);
+    weight = __uint_as_float(head[0]);
+    best = __uint_as_float(head[1]);
 }
 // Whether this workgroup is the last of others + 1 to come here; it leaves the count at 0.  Parts were written through: once
 // every wave's stores have been acknowledged and all waves have come, the count may say so.
@@ -459,7 +463,7 @@ __device__ __forceinline__ bool last_to_come(int* count, int others, int* last_o
 // Parts w_first .. w_last of a unit, this workgroup's among them and written, become its result: in two steps, sixteen
 // consecutive ones and then the sixteens, so that a workgroup reads at most 16 + 64 of them.  A column's quads are neighbouring
 // lanes: all of them have read a part before one writes the sixteen's sum in its place.
-template <int D, int COLUMNS, int THREADS, bool WIDE, bool MASK, class Finish>
+template <int D, int COLUMNS, int THREADS, bool MASK, class Finish>
 __device__ void join_parts(float* parts, int* done, int w_first, int w_last, int columns, int* last_one, Finish finish) {
     constexpr int QUADS = D / 4;
     const int group = ((int)blockIdx.x - w_first) >> 4, g_first = w_first + 16 * group, g_last = min(g_first + 15, w_last), groups = (w_last - w_first >> 4) + 1;
@@ -488,7 +492,7 @@ __device__ void join_parts(float* parts, int* done, int w_first, int w_last, int
                     const int ww = min(w + k * step, to);                      // (those past the end are read twice and not used)
 #pragma unroll
                     for (int u = 0; u < AT_ONCE; ++u)
-                        get_part<D, COLUMNS, WIDE>(parts, 2 * (long long)ww + (ww == w_first), col[u], c[u], in[u][k], in_weight[u][k], in_best[u][k]);
+                        get_part<D, COLUMNS>(parts, 2 * (long long)ww + (ww == w_first), col[u], c[u], in[u][k], in_weight[u][k], in_best[u][k]);
                 }
 #pragma unroll
                 for (int k = 0; k < PARTS; ++k)
@@ -507,14 +511,13 @@ __device__ void join_parts(float* parts, int* done, int w_first, int w_last, int
             for (int u = 0; u < AT_ONCE; ++u)
                 if (AT_ONCE == 1 || i0 + u * THREADS < columns * QUADS) {
                     if (final) finish(col[u], c[u], y[u], weight[u]);
-                    else put_part<D, COLUMNS, WIDE>(parts, 2 * (long long)from + (from == w_first), col[u], c[u], y[u], weight[u], best[u]);
+                    else put_part<D, COLUMNS>(parts, 2 * (long long)from + (from == w_first), col[u], c[u], y[u], weight[u], best[u]);
                 }
         }
     };
     const auto join = [&](int from, int to, int step, bool final) {
         using std::integral_constant;
-        if (WIDE && (to - from) / step < 2 && columns * QUADS > 2 * THREADS) join_some(integral_constant<int, 4>(), integral_constant<int, 2>(), from, to, step, final);
-        else if (MASK && (to - from) / step < 4 && columns * QUADS > THREADS) join_some(integral_constant<int, 2>(), integral_constant<int, 4>(), from, to, step, final);
+        if (MASK && (to - from) / step < 4 && columns * QUADS > THREADS) join_some(integral_constant<int, 2>(), integral_constant<int, 4>(), from, to, step, final);
         else join_some(integral_constant<int, 1>(), integral_constant<int, 8>(), from, to, step, final);
     };
     if (g_last > g_first) {
@@ -1080,11 +1083,11 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
                     weight += f * wsum[w][l];
                 }
             if (complete) finish(col, c, y, weight);
-            else put_part<D, kColumns, false>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
+            else put_part<D, kColumns>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
         }
         if (complete) continue;
         const part_range parts = parts_of<kSnap>(unit_at, size, part);
-        join_parts<D, kColumns, 256, false, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
+        join_parts<D, kColumns, 256, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
     // rows that see nothing: no unit holds them
     const int width = a.g * a.v.heads * QUADS;
@@ -1189,7 +1192,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
         const int at = w * part;
         if (at >= total || w == 0) return min(at, total);
         const int ti = tile_at(at), size = uniform(a.tile[2 * ti + 1].w), in = at - uniform(a.tile_at[ti]);
-        return snapped<kTileSnap>(at, in - divide(in, size) * size, size);
+        return snapped<kTileSnap<MASK>>(at, in - divide(in, size) * size, size);
     };
     const int end = boundary(blockIdx.x + 1);
     int at = boundary(blockIdx.x);
@@ -1215,8 +1218,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
     for (; at < end; unit_at = at, ti += head + 1 == a.v.heads, head = head + 1 == a.v.heads ? 0 : head + 1) {
         const int4 e = a.tile[2 * ti], t = a.tile[2 * ti + 1];
         const int slot = uniform(e.x), len = uniform(e.y), row0 = uniform(e.z), rows = uniform(e.w);
-        const int which = uniform(t.x), tile_lo = uniform(t.y), tile_n = uniform(t.z), size = uniform(t.w), grains = size - kTileCost;
-        const int from = max(at - unit_at - kTileCost, 0), to = min(min(size, end - unit_at) - kTileCost, grains);
+        const int which = uniform(t.x), tile_lo = uniform(t.y), tile_n = uniform(t.z), size = uniform(t.w), grains = size - kTileCost<MASK>;
+        const int from = max(at - unit_at - kTileCost<MASK>, 0), to = min(min(size, end - unit_at) - kTileCost<MASK>, grains);
         at = unit_at + size;
         const bool begins = from == 0, complete = begins && to == grains;
         // stages; MASK: of those that are not left out
@@ -1516,7 +1519,58 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
             put_out(a.Y, (long long)(row0 + j0 + j) * a.Y.stride + (long long)(head * a.g + x - j * a.g) * D + c,
                     weight == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : y * __builtin_amdgcn_rcpf(weight));
         };
-        if (complete) {
+        bool whole = complete;
+        if constexpr (MASK) {
+            if (!complete) {
+                constexpr int QUAD = 4 * OT;
+                float best = top > -kFar ? top * kappa : -kFar;
+                const auto quads = [&](f32x4 (&y)[QUAD]) {
+#pragma unroll
+                    for (int i = 0; i < QUAD; ++i) y[i] = f32x4{o[i / 4][4 * (i % 4)], o[i / 4][4 * (i % 4) + 1], o[i / 4][4 * (i % 4) + 2], o[i / 4][4 * (i % 4) + 3]};
+                };
+                const auto put = [&](long long slot) {
+                    f32x4 y[QUAD];
+                    quads(y);
+                    put_tile<D>(a.parts, slot, y, sum, best, hh == 0, column);
+                };
+                put(2 * (long long)blockIdx.x + begins);
+                const part_range parts = parts_of<kTileSnap<MASK>>(unit_at, size, part);
+                // as join_parts does it: sixteen consecutive parts and then the sixteens, but in the lanes that hold a part anyway
+                const int group = ((int)blockIdx.x - parts.first) >> 4, g_first = parts.first + 16 * group, g_last = min(g_first + 15, parts.last), groups = (parts.last - parts.first >> 4) + 1;
+                const auto merge = [&](int from, int to, int step) {
+                    best = -kFar;
+                    sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < OT; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) o[i][k] = 0.f;
+                    for (int w = from; w <= to; w += step) {
+                        f32x4 in[QUAD];
+                        float in_weight, in_best;
+                        get_tile<D>(a.parts, 2 * (long long)w + (w == parts.first), in, in_weight, in_best, column);
+                        const float now = fmaxf(best, in_best);
+                        const float f = best == now ? 1.f : __builtin_amdgcn_exp2f(best - now), f2 = in_best == now ? 1.f : __builtin_amdgcn_exp2f(in_best - now);
+#pragma unroll
+                        for (int i = 0; i < QUAD; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) o[i / 4][4 * (i % 4) + k] = o[i / 4][4 * (i % 4) + k] * f + in[i][k] * f2;
+                        sum = sum * f + in_weight * f2;
+                        best = now;
+                    }
+                };
+                whole = true;
+                if (g_last > g_first) {
+                    whole = last_to_come(&a.done[2 * g_first], g_last - g_first, &last_one);
+                    if (whole) merge(g_first, g_last, 1);
+                }
+                if (whole && groups > 1) {
+                    if (g_last > g_first) put(2 * (long long)g_first + (g_first == parts.first));
+                    whole = last_to_come(&a.done[2 * parts.first + 1], groups - 1, &last_one);
+                    if (whole) merge(parts.first, parts.first + 16 * (groups - 1), 16);
+                }
+            }
+        }
+        if (whole) {
             // a column's channels lie in 16 pieces of 8 bytes over its two lanes: through LDS (this wave's own 32 rows of it, the
             // buffers are done with), so that rows go out whole
             const float over = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum);  // (where the sum is 0, so is the column)
@@ -1549,18 +1603,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                     for (int k = 0; k < 4; ++k)
                         put_out(a.Y, y_at + 32 * ot + 8 * k, f32x4{o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]} * over);
             }
-        } else if (real) {
+        } else if (!MASK && real) {
             const float best = top > -kFar ? top * kappa : -kFar;
 #pragma unroll
             for (int ot = 0; ot < OT; ++ot)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    put_part<D, kTile, MASK>(a.parts, 2 * (long long)blockIdx.x + begins, column, 32 * ot + 8 * k + 4 * hh,
+                    put_part<D, kTile>(a.parts, 2 * (long long)blockIdx.x + begins, column, 32 * ot + 8 * k + 4 * hh,
                                        f32x4{o[ot][4 * k], o[ot][4 * k + 1], o[ot][4 * k + 2], o[ot][4 * k + 3]}, sum, best);
         }
-        if (complete) continue;
-        const part_range parts = parts_of<kTileSnap>(unit_at, size, part);
-        join_parts<D, kTile, kTileThreads, MASK, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
+        if (MASK || complete) continue;
+        const part_range parts = parts_of<kTileSnap<MASK>>(unit_at, size, part);
+        join_parts<D, kTile, kTileThreads, false>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
 }
 
@@ -1595,7 +1649,7 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     const double units = ((double)a.rows.R * a.g / kColumns + a.rows.n) * a.v.heads, tiles = ((double)a.rows.R * a.g / kTile + a.rows.n) * a.v.heads;
     const double blocks = (double)((long long)a.v.max_pages << a.v.page_shift);
     while (units * (blocks / (1 << a.grain) + kUnitCost + 1) > 1e9 && a.grain < 26) ++a.grain;
-    while (tiles * (blocks / 2 / (1 << a.tile_grain) + kTileCost + 1) > 1e9 && a.tile_grain < 25) ++a.tile_grain;
+    while (tiles * (blocks / 2 / (1 << a.tile_grain) + kTileCost<MASK> + 1) > 1e9 && a.tile_grain < 25) ++a.tile_grain;
     const bool prompts = may_have_prompts(x_dtype, a.g, a.rows);
     if (prompts) {
         const size_t n = tile_count(a.g, a.rows);
