@@ -107,6 +107,8 @@ constexpr int kLittle = 8192;
 // share, and a quarter of the steps one after another.  Trees of 26 rows (28 heads on 4), us with 64 and with 16: one of 500 tokens (of 16 rows) 28, 14; 8 of 1000 44, 23;
 // 16 of 1000 46, 30; fp32 (8 heads of 64, 63 rows) one of 600 43, 17, but 64 of them, 12800 long, 74 and 90.
 constexpr int kNarrow = 16;
+// Masks: where every workgroup can have one unit's part alone it does not begin another's behind it, which costs it about kAligned blocks more.
+constexpr int kAligned = 16;
 
 // With sinks (MASK) the blocks that hold them come first and lo more are left out behind them: block i of an entry's is i, or lo + i from sink_blocks on.
 template <bool MASK>
@@ -129,6 +131,7 @@ struct attn_list {
     int* at;                   // [n + 1]
     int2 *who, *rows;          // [n] slot and len; row0 and rows (null: one row each)
     int even;                  // > 0: every unit counts as this long
+    int part;                  // and, where that is several workgroups' (masks), each takes this much of it
     bool prompts;              // entries of many rows are the prompt kernel's
     int width;                 // columns of a unit
     bool blank;                // there are entries of more than kBlank rows that see nothing
@@ -149,7 +152,7 @@ template <bool F32, bool OWN_ROWS, bool MASK>
 __device__ attn_list make_list(const attn_args& a, void* lds) {                // 256 threads
     __shared__ int waves[5][4];
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
-    attn_list l{(int*)((int2*)lds + (OWN_ROWS ? 2 * n : n)), (int2*)lds, OWN_ROWS ? (int2*)lds + n : nullptr, 0, false, kColumns, false};
+    attn_list l{(int*)((int2*)lds + (OWN_ROWS ? 2 * n : n)), (int2*)lds, OWN_ROWS ? (int2*)lds + n : nullptr, 0, 0, false, kColumns, false};
     if (OWN_ROWS && ((!F32 && a.tiles) || MASK)) {                         // every workgroup finds the same
         int work = 0;
         for (int b = lo; b < hi; ++b) {
@@ -223,7 +226,16 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
         total_units += waves[1][w];
         longest = max(longest, waves[2][w]);
     }
-    l.even = uniform(total_units <= (int)gridDim.x && longest <= kShort && a.grain == 0 ? longest : 0);
+    l.even = l.part = uniform(total_units <= (int)gridDim.x && longest <= kShort && a.grain == 0 ? longest : 0);
+    if (MASK && l.even == 0 && total_units > 0 && total_units <= (int)gridDim.x && a.grain == 0) {
+        // as many workgroups a unit as there are for each, if that is not much longer than equal parts
+        const int units = uniform(total_units), most = uniform(longest), each = divide((int)gridDim.x, units);
+        const int part = max(divide(most + each - 1, each), a.least), equal = max(divide(uniform(total), (int)gridDim.x) + 1, a.least);
+        if (part <= equal + (OWN_ROWS && l.width == kColumns ? kUnitCost : kAligned)) {
+            l.part = part;
+            l.even = divide(most + part - 1, part) * part;
+        }
+    }
     for (int b = lo; b < hi; ++b) {
         const int4 e = l.entry(b);
         const entry_span s = span_of<MASK>(a, e.y, e.w, l.width);
@@ -928,7 +940,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
     const attn_list list = make_list<F32, OWN_ROWS, MASK>(a, list_lds);
     if (OWN_ROWS && a.tiles && blockIdx.x == gridDim.x - 1) plan_tiles<MASK>(a, list);
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), h = lane >> 4;
-    const int total = uniform(list.at[a.rows.n]), part = list.even ? list.even : max(divide(total, (int)gridDim.x) + 1, a.least);
+    const int total = uniform(list.at[a.rows.n]), part = list.even ? uniform(list.part) : max(divide(total, (int)gridDim.x) + 1, a.least);
     const auto over_g = [&](int x) { return a.g == 1 ? x : (int)__umulhi((unsigned)x, a.g_inverse); };
     struct place {
         int4 entry;
@@ -1086,7 +1098,7 @@ __global__ __launch_bounds__(256, kStreamsPerCu<D>) void kv_attn_stream_kernel(a
             else put_part<D, kColumns>(a.parts, 2 * blockIdx.x + begins, col, c, y, weight, best);
         }
         if (complete) continue;
-        const part_range parts = parts_of<kSnap>(unit_at, size, part);
+        const part_range parts = MASK && list.even ? part_range{divide(unit_at, part), divide(unit_at + kUnitCost + grains - 1, part)} : parts_of<kSnap>(unit_at, size, part);
         join_parts<D, kColumns, 256, MASK>(a.parts, a.done, parts.first, parts.last, columns, &last_one, finish);
     }
     // rows that see nothing: no unit holds them
@@ -1650,7 +1662,9 @@ static hipError_t run(hipStream_t st, attn_args a, void* ws, int x_dtype) {
     const double blocks = (double)((long long)a.v.max_pages << a.v.page_shift);
     while (units * (blocks / (1 << a.grain) + kUnitCost + 1) > 1e9 && a.grain < 26) ++a.grain;
     while (tiles * (blocks / 2 / (1 << a.tile_grain) + kTileCost<MASK> + 1) > 1e9 && a.tile_grain < 25) ++a.tile_grain;
-    const bool prompts = may_have_prompts(x_dtype, a.g, a.rows);
+    // Calls that are little work however long their sequences are launch no second kernel, which without a tile takes 4.5 us.
+    const double longest = ((double)((long long)a.rows.R * a.g / kColumns) + a.rows.n) * a.v.heads * (a.v.max_len / kKvBlock + kUnitCost);
+    const bool prompts = may_have_prompts(x_dtype, a.g, a.rows) && longest > kLittle;
     if (prompts) {
         const size_t n = tile_count(a.g, a.rows);
         a.tile = (int4*)ws;
