@@ -468,7 +468,7 @@ essa_status essa_kv_free(essa_ctx* ctx, essa_kv* kv, const int32_t* seqs, int n)
  * first len - c ones, the length becomes len - c + keep[b], and pages past it go back.  Their 4-bit values are moved as they are.
  * Not served (ESSA_KV_BAD_ENTRY, the sequence is as it was): a sequence past max_seqs or named twice (from the second on), keep[b] not in [0, c], more rows
  * than the sequence has tokens, a path that does not ascend or leaves the entry's rows, a page of these rows that another sequence holds too.
- *   path DEVICE int32 [R]    keep DEVICE int32 [n]    served DEVICE int32 [n] or NULL: seqs[b], or why not */
+ *   path DEVICE int32 [R]    keep DEVICE int32 [n]    served DEVICE int32 [n] (the batch's seqs, if so wanted) or NULL: seqs[b], or why not */
 essa_status essa_kv_accept(essa_ctx* ctx, essa_kv* kv, const essa_kv_batch* batch, const int32_t* path, const int32_t* keep, int32_t* served);
 /* Moves the pages in use into pages 0 .. used - 1: those at or above `used` go, in ascending order, to the free ones
  * below it; table and refs follow.

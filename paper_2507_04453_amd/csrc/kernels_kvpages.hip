@@ -88,7 +88,7 @@ __global__ void kv_clear_kernel(int32_t* table, long long entries, int32_t* len,
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < entries; i += step) table[i] = -1;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < max_seqs; i += step) len[i] = 0;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < 2 * essa_k::kKvAttnWorkgroups; i += step) done[i] = 0;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < max_seqs; i += step) come[i] = 0;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i <= max_seqs; i += step) come[i] = 0;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n_pages; i += step) refs[i] = 0;
 }
 
@@ -315,7 +315,6 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(pages_view v, essa_k::kv
     __shared__ unsigned char codes[kKvBlock][D + 4];
     const int b = blockIdx.x;
     const accept_entry e = accept_of(v, rows, path, keep, b);
-    if (served && blockIdx.y == 0 && threadIdx.x == 0) served[b] = e.ok;
     const bool moves = e.ok >= 0 && e.moved < e.keep;
     const int tok = threadIdx.x / 8, part = threadIdx.x % 8, per_page = v.page_tokens / kKvBlock;
     const auto block_at = [&](int head, int block) {
@@ -387,6 +386,18 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(pages_view v, essa_k::kv
         }
         __syncthreads();
         if (!last) return;
+    }
+    if (served) {                                              // may be the list of sequences itself: written by the last entry, when nobody reads that any more
+        __shared__ bool last_entry;
+        if (threadIdx.x == 0) {
+            __hip_atomic_store(&v.s.entry_ok[b], e.ok, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            last_entry = atomicAdd(&v.s.come[v.max_seqs], 1) == (int)gridDim.x - 1;
+            if (last_entry) v.s.come[v.max_seqs] = 0;
+        }
+        __syncthreads();
+        if (last_entry)
+            for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) served[i] = __hip_atomic_load(&v.s.entry_ok[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     if (e.ok < 0) return;
     const int now = e.base + e.keep;
@@ -474,7 +485,7 @@ pages_view view_of(const essa_kv* kv) {
 namespace essa_k {
 
 size_t kv_scratch_words(const essa_kv_desc& d) {
-    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4 + 2 * kKvAttnWorkgroups + d.max_seqs;
+    return 2 * (size_t)d.n_pages + 3 * (size_t)d.max_seqs + std::max((size_t)d.max_seqs * d.max_pages, (size_t)d.n_pages) + 4 + 2 * kKvAttnWorkgroups + d.max_seqs + 1;
 }
 kv_scratch kv_scratch_of(const essa_kv* kv) {
     const essa_kv_desc& d = kv->d;
@@ -487,7 +498,7 @@ kv_scratch kv_scratch_of(const essa_kv* kv) {
     s.count = s.entry_ok + d.max_seqs;
     s.done = s.count + 4;
     s.come = s.done + 2 * kKvAttnWorkgroups;
-    s.rows = s.come + d.max_seqs;
+    s.rows = s.come + d.max_seqs + 1;
     return s;
 }
 

@@ -63,7 +63,7 @@ struct kv_scratch {
     int32_t* rows;             // [max_seqs, max_pages]
     int32_t* count;            // [4]
     int32_t* done;             // [2 kKvAttnWorkgroups] attention's counts of finished parts, 0 between calls
-    int32_t* come;             // [max_seqs] workgroups of an entry that have moved their heads' tokens (accept), 0 between calls
+    int32_t* come;             // [max_seqs + 1] workgroups of an entry that have moved their heads' tokens (accept), and entries that all have; 0 between calls
 };
 inline int kv_max_len(const essa_kv_desc& d) { return (d.max_pages < d.n_pages ? d.max_pages : d.n_pages) * d.page_tokens; }
 size_t kv_scratch_words(const essa_kv_desc& d);

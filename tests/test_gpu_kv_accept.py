@@ -148,6 +148,26 @@ def test_spoiled_lengths_and_tables(essa, ctx, layers):
     kv.close()
 
 
+def test_answers_in_place_of_the_sequences(essa, ctx):
+    """served is the batch's own list: answers are those of a list apart, every time (names twice behind refused ones among them)."""
+    n = 600
+    g = np.random.default_rng(9)
+    out = []
+    names = [int(x) for x in g.integers(-1, 320, n)]
+    keep = [int(x) for x in g.integers(-1, 3, n)]
+    for turn in range(6):
+        p = Pair(essa, ctx, 1500, 32, 300 + n, 128, layers=3, hkv=2)
+        p.extend(list(range(300)), [40] * 300)
+        seqs, served = i32(names), i32([9] * n)
+        batch = essa.KvBatch(seqs, starts([2] * n), 2 * n)
+        essa.essa_kv_accept(ctx, p.kv, batch, i32([0, 1] * n), i32(keep), seqs if turn % 2 else served)
+        out.append((seqs if turn % 2 else served).tolist())
+        want = p.model.accept(names, [2] * n, [[0, 1]] * n, keep)
+        assert out[-1] == want
+        p.check()
+        p.kv.close()
+
+
 def test_many_sequences(essa, ctx):
     n = 900
     p = Pair(essa, ctx, 5000, 32, n, 128, layers=1, hkv=1)
