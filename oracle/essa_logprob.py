@@ -38,7 +38,7 @@ def token_logprobs_limits(logits, scale=1.0):
 
     In single precision, u = 2^-24.  An exponent d = k x + down is rounded once (u |d|), its factor k = scale log2(e) twice (2 u of
     |x - max| k, as what is common to a row cancels), exp2 and log2 are right to 2 u; a lane adds V / 256 weights at most, the row
-    16 sums more, each of which rounds.  So with A = sum p |z - max| + 8 (8: what a lane's `down` may be short of its maximum by, in
+    16 sums more, each of which rounds.  So with A = sum p |z - max| + 8 (8: what a wave's `down` may be short of its maximum by, in
     exponents of 2) the weights' sum is off by ((V / 256 + 20) + 4 A) u of itself, its logarithm by as much and 2 u of itself, and the sum of weights
     times exponents by ((V / 256 + 24) + 4) u A and 4 u times the sum of p (z - max)^2."""
     x = np.asarray(logits, np.float64)

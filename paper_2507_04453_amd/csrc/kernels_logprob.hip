@@ -3,7 +3,11 @@
 // With k = scale log2(e) and any number `down` (about -k max x), the weights 2^d, d = k x + down, give
 //   s = sum 2^d,  t = sum d 2^d:    log2 p_j = d_j - log2 s,    entropy / ln 2 = log2 s - t / s,
 // whatever `down` was rounded to, as long as all of a row use the same; sums of another `down` become this one's by
-// f = 2^(change), s f and f (t + change s).  Every lane keeps its own, and moves it when a value passes its weights' 2^kSlack.
+// f = 2^(change), s f and f (t + change s).  A wave has one, and moves it when a value's weight passes 2^kSlack, which after its first load is rare.
+// A value that moved it stays out of the sums (`peak`) until the next: where it is the row's largest after all, and all but certain, what is left of the
+// others is a small number of its own, not the last bits of 1 + it, and with a = s / 2^d_peak and b = (t - d_peak s) / 2^d_peak
+//   - log p_peak = log(1 + a),    entropy = log(1 + a) - ln 2 b / (1 + a)
+// are right to the last bits of themselves.
 #include <algorithm>
 
 #include "forward_device.h"
@@ -27,7 +31,9 @@ __device__ __forceinline__ uint32_t ordered(float x) {         // as x is; -0 is
 
 struct row_sums {
     float max, down, s, t;
+    float peak;                // a value whose weight is not in s and t; -inf: there is none
 };
+constexpr float kNone = -INFINITY;
 __device__ __forceinline__ float down_of(float max, float k) {
     const float z = max * k;
     return z > kHuge ? -kHuge : z >= -kHuge ? -z : kHuge;      // nothing seen (-inf): kHuge
@@ -37,6 +43,14 @@ __device__ __forceinline__ void move_to(row_sums& a, float down) {
     a.t = f * (a.t + fmaxf(change, -2.f * kHuge) * a.s);
     a.s *= f;
     a.down = down;
+}
+
+__device__ __forceinline__ void take_peak(row_sums& a, float k) {              // into the sums
+    if (a.peak == kNone) return;
+    const float d = fmaf(a.peak, k, a.down), e = __builtin_amdgcn_exp2f(d);
+    a.s += e;
+    a.t = fmaf(e, fmaxf(d, -256.f), a.t);
+    a.peak = kNone;
 }
 
 // A row in memory: loads are of whole 16 bytes, so a row that begins inside of them begins `skip` values into its first load.
@@ -113,7 +127,7 @@ __device__ __forceinline__ float wave_max(float x) { return neighbours_max<64>(x
 __device__ __forceinline__ float wave_sum(float x) { return neighbours<64>(x, [](float a, float b) { return a + b; }); }
 // all threads' sums as one, everywhere; waves: LDS
 template <int W>
-__device__ void join_threads(row_sums& a, float k, float (&waves)[3][W]) {
+__device__ void join_threads(row_sums& a, float k, float (&waves)[4][W]) {
     const int wave = threadIdx.x / 64;
     const float max = wave_max(a.max);
     if ((threadIdx.x & 63) == 0) waves[0][wave] = max;
@@ -121,18 +135,29 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[3][W]) {
     a.max = waves[0][0];
 #pragma unroll
     for (int w = 1; w < W; ++w) a.max = fmaxf(a.max, waves[0][w]);
+    if (a.peak != a.max) take_peak(a, k);
     move_to(a, down_of(a.max, k));
     const float s = wave_sum(a.s), t = wave_sum(a.t);
+    const int peaks = __popcll(__ballot(a.peak != kNone));
     if ((threadIdx.x & 63) == 0) {
         waves[1][wave] = s;
         waves[2][wave] = t;
+        waves[3][wave] = (float)peaks;
     }
     __syncthreads();
     a.s = a.t = 0.f;
+    float all = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         a.s += waves[1][w];
         a.t += waves[2][w];
+        all += waves[3][w];
+    }
+    a.peak = all > 0.f ? a.max : kNone;
+    if (all > 1.f) {                                           // of equal ones one stays out
+        const float d = fmaf(a.max, k, a.down), e = (all - 1.f) * __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        a.t = fmaf(e, d, a.t);
     }
     __syncthreads();
 }
@@ -392,11 +417,11 @@ __device__ __forceinline__ given given_of(const logprob_args& a, const row_view<
     return g;
 }
 template <bool F32, bool TOP, int T>
-__device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, given first, const float* seg, int segments, float (&waves)[3][T / 64],
+__device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, given first, const float* seg, int segments, float (&waves)[4][T / 64],
                            top_lds<T>* l) {
     const bool huge = fabsf(r.max) <= 3.402823466e38f && !(fabsf(r.max * a.k) <= kHuge);
     if (huge) {
-        row_sums mine{r.max, 0.f, 0.f, 0.f};
+        row_sums mine{r.max, 0.f, 0.f, 0.f, kNone};
         for (int i = v.skip + (int)threadIdx.x; i < v.n; i += T) {
             const float d = (v.value(i) - r.max) * a.k, e = __builtin_amdgcn_exp2f(d);
             mine.s += e;
@@ -410,6 +435,7 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
         }
         __syncthreads();
         r.s = r.t = 0.f;
+        r.peak = kNone;
 #pragma unroll
         for (int w = 0; w < T / 64; ++w) {
             r.s += waves[1][w];
@@ -418,9 +444,18 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
     }
     const bool nothing = r.max == -INFINITY && r.s == 0.f, bad = !(r.s == r.s) || r.max == INFINITY;
     constexpr float kLn2 = 0.693147180559945309f;
-    const float log_s = __builtin_amdgcn_logf(r.s);
-    // from the largest value on, whose weight is 2^(k max + down): about 1.  Any logit that fp32 holds has a log probability then, if fp32 holds that.
-    const float most = ((huge ? 0.f : fmaf(r.max, a.k, r.down)) - log_s) * kLn2;
+    // the largest value's log probability, from which every other is a difference of logits away, and the entropy
+    const float d = huge ? 0.f : fmaf(r.max, a.k, r.down);
+    float most, entropy;
+    if (r.peak != kNone) {
+        const float over = __builtin_amdgcn_exp2f(-d), rest = r.s * over;
+        most = -log1pf(rest);
+        entropy = -most - kLn2 * (r.t - d * r.s) * over / (1.f + rest);
+    } else {
+        const float ln_s = logf(r.s);
+        most = d * kLn2 - ln_s;
+        entropy = ln_s - r.t / r.s * kLn2;
+    }
     const auto logp = [&](float x) {
         if (bad) return __uint_as_float(0x7fc00000u);
         if (nothing || x == -INFINITY) return -INFINITY;
@@ -430,7 +465,7 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
         const given g = i < T ? first : given_of<F32>(a, v, row, i);
         a.logp[(size_t)row * a.n_tokens + i] = g.what == 0 ? 0.f : g.what == 2 ? logp(g.x) : __uint_as_float(0x7fc00000u);
     }
-    if (a.entropy && threadIdx.x == 0) a.entropy[row] = bad ? __uint_as_float(0x7fc00000u) : nothing ? 0.f : (log_s - r.t / r.s) * kLn2;
+    if (a.entropy && threadIdx.x == 0) a.entropy[row] = bad ? __uint_as_float(0x7fc00000u) : nothing ? 0.f : entropy;
     if constexpr (TOP) {
         int32_t* ids = a.top_ids + (size_t)row * a.n_top;
         float* lps = a.top_logp + (size_t)row * a.n_top;
@@ -452,7 +487,7 @@ template <bool F32, bool TOP, int T>
 __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
     extern __shared__ float seg[];                             // [segments of this part], then of the row
     constexpr int W = T / 64;
-    __shared__ float waves[3][W];
+    __shared__ float waves[4][W];
     __shared__ top_lds<T> top;
     __shared__ int last_one;
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
@@ -462,7 +497,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
     constexpr int PER = kLoad / kLogprobSegment;               // segments of a load
 
     const given first = given_of<F32>(a, v, row, threadIdx.x);                 // asked for before the row, or they would be waited for at the end
-    row_sums r{-INFINITY, kHuge, 0.f, 0.f};
+    row_sums r{-INFINITY, kHuge, 0.f, 0.f, kNone};
     const auto take = [&](int j, const raw_values<F32>& raw) {
         float x[kVec];
         unpack<F32>(v, j, lane, raw, x);
@@ -487,7 +522,19 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
         most = fmaxf(most, half);
         r.max = fmaxf(r.max, most);
         if (__any(fmaf(most, a.k, r.down) > kSlack)) {
-            if (fmaf(most, a.k, r.down) > kSlack) move_to(r, -(most * a.k));
+            const float now = wave_max(most);
+            take_peak(r, a.k);
+            move_to(r, -(now * a.k));
+            if (most == now) {
+                r.peak = now;
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    const bool it = x[i] == now && !found;
+                    found |= it;
+                    x[i] = it ? -INFINITY : x[i];
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
@@ -516,6 +563,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
             __hip_atomic_store(mine, r.max, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             __hip_atomic_store(mine + 1, r.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             __hip_atomic_store(mine + 2, r.t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(mine + 3, r.peak, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         float* row_seg = a.segments + (size_t)row * a.row_segments;
         if constexpr (TOP)
@@ -530,12 +578,13 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
         }
         __syncthreads();
         if (!last_one) return;
-        r = row_sums{-INFINITY, kHuge, 0.f, 0.f};
+        r = row_sums{-INFINITY, kHuge, 0.f, 0.f, kNone};
         if ((int)threadIdx.x < a.parts) {
             const float* p = a.sums + ((size_t)row * a.parts + threadIdx.x) * 4;
             r.max = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             r.s = __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             r.t = __hip_atomic_load(p + 2, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            r.peak = __hip_atomic_load(p + 3, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             r.down = down_of(r.max, a.k);
         }
         if constexpr (TOP)

@@ -115,6 +115,48 @@ def test_sharp_and_flat_rows(essa, ctx, dtype, R):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,V", [(5, 3000), (3, 60000), (200, 9000), (520, 9000)])
+def test_tokens_that_are_all_but_certain(essa, ctx, dtype, R, V):
+    """The log probability of a token far ahead of all others, and the entropy of its row, to the last bits of themselves: with G the exponents of 2 that others
+    are behind (those that count), a weight is off by 6 G u at most (its exponent's rounding and twice its factor's), their sum by V / 256 + 20 more, what
+    is made of it by 8 u."""
+    g = np.random.default_rng(40)
+    at = g.integers(0, V, R)
+    lead = np.where(np.arange(R) % 3 == 0, 12.0, np.where(np.arange(R) % 3 == 1, 20.0, 30.0))
+
+    def edit(x):
+        x[np.arange(R), at] = 9.0 + lead
+    x, view = _logits(R, V, dtype, 41, edit=edit)
+    out = _check(essa, ctx, x, view, np.stack([at, (at + 1) % V], 1), 2)
+    z = x - x.max(1, keepdims=True)
+    z[np.arange(R), at] = -np.inf
+    rest = np.exp(z).sum(1)
+    G = ((x.max(1) - np.sort(x, 1)[:, -2]) + 8) / np.log(2)              # what is 8 nats behind the first of them counts for little
+    far = -(np.exp(z) * np.where(np.isfinite(z), z, 0)).sum(1)
+    h = np.log1p(rest) + far / (1 + rest)
+    limit = (V / 256 + 28 + 6 * G) * 2.0 ** -24
+    lp, got = host(out["logp"])[:, 0], host(out["entropy"])
+    assert (np.abs(lp + np.log1p(rest)) <= limit * rest).all(), np.max(np.abs(lp + np.log1p(rest)) / rest / limit)
+    assert (np.abs(got - h) <= 2 * limit * h).all(), np.max(np.abs(got - h) / h / limit)
+    assert out["top_ids"][:, 0].tolist() == at.tolist() and np.array_equal(host(out["top_logp"])[:, 0], lp)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R", [3, 200, 530])
+def test_two_or_more_largest_ones(essa, ctx, dtype, R):
+    """The largest value several times, in one lane's load, in different lanes, waves and parts: none of them is lost or counted twice."""
+    V = 9000
+
+    def edit(x):
+        for i in range(R):
+            x[i, [0, 1, 700, 8999][:i % 4 + 1]] = 40.0
+            if i % 5 == 0:
+                x[i, 512:520] = 40.0
+    x, view = _logits(R, V, dtype, 42, edit=edit)
+    _check(essa, ctx, x, view, np.tile([0, 1, 5], (R, 1)), 3)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("R,V", [(4, 700), (4, 40000), (515, 3000), (515, 6000), (200, 40000), (515, 66000)])
 def test_equal_logits_come_in_order(essa, ctx, dtype, R, V):
     """Few levels, so that almost everything is a tie: the lower tokens are taken, and -0 equals 0."""
