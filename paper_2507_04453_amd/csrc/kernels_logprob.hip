@@ -21,8 +21,10 @@ using essa_k::logprob_args;
 constexpr int kVec = 8;                        // values of a lane's load (two loads in fp32)
 constexpr int kLoad = 64 * kVec;               // values of a wave's
 constexpr float kSlack = 8.f;
-// What `down` is where a lane has seen nothing that counts.  Rows whose largest k x is beyond +-kHuge have sums of their own (see finish_row).
-constexpr float kHuge = 1e37f;
+// What `down` is where a lane has seen nothing that counts: values with k x below -kHuge have no weight.  As `down` is rounded to half a step of
+// k max x, the largest values' weights are 2^(that error): 4 at kHuge, past all numbers at 1e30.  So rows whose largest k x is beyond +-kHuge have sums of
+// their own (see finish_row).
+constexpr float kHuge = 67108864.f;
 
 __device__ __forceinline__ uint32_t ordered(float x) {         // as x is; -0 is 0
     const int b = __float_as_int(x + 0.f);
@@ -34,8 +36,15 @@ struct row_sums {
     float peak;                // a value whose weight is not in s and t; -inf: there is none
 };
 constexpr float kNone = -INFINITY;
+// Rounded, wherever it goes: the compiler makes one instruction of a product and a sum, and a difference from the exact product is another one, by up to 4
+// exponents.
+__device__ __forceinline__ float scaled(float x, float k) {
+    float z = x * k;
+    asm("" : "+v"(z));
+    return z;
+}
 __device__ __forceinline__ float down_of(float max, float k) {
-    const float z = max * k;
+    const float z = scaled(max, k);
     return z > kHuge ? -kHuge : z >= -kHuge ? -z : kHuge;      // nothing seen (-inf): kHuge
 }
 __device__ __forceinline__ void move_to(row_sums& a, float down) {
@@ -419,28 +428,34 @@ __device__ __forceinline__ given given_of(const logprob_args& a, const row_view<
 template <bool F32, bool TOP, int T>
 __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int row, row_sums r, given first, const float* seg, int segments, float (&waves)[4][T / 64],
                            top_lds<T>* l) {
-    const bool huge = fabsf(r.max) <= 3.402823466e38f && !(fabsf(r.max * a.k) <= kHuge);
+    const bool huge = fabsf(r.max) <= 3.402823466e38f && !(fabsf(scaled(r.max, a.k)) <= kHuge);
     if (huge) {
-        row_sums mine{r.max, 0.f, 0.f, 0.f, kNone};
+        float s = 0.f, t = 0.f, largest = 0.f;                 // relative to the maximum, of which one stays out
         for (int i = v.skip + (int)threadIdx.x; i < v.n; i += T) {
-            const float d = (v.value(i) - r.max) * a.k, e = __builtin_amdgcn_exp2f(d);
-            mine.s += e;
-            mine.t = fmaf(e, fmaxf(d, -256.f), mine.t);
+            const float x = v.value(i), d = (x - r.max) * a.k, e = __builtin_amdgcn_exp2f(d);
+            largest += x == r.max ? 1.f : 0.f;
+            s += x == r.max ? 0.f : e;
+            t = fmaf(e, fmaxf(d, -256.f), t);
         }
-        const float s = wave_sum(mine.s), t = wave_sum(mine.t);
+        s = wave_sum(s);
+        t = wave_sum(t);
+        largest = wave_sum(largest);
         __syncthreads();
         if ((threadIdx.x & 63) == 0) {
             waves[1][threadIdx.x / 64] = s;
             waves[2][threadIdx.x / 64] = t;
+            waves[3][threadIdx.x / 64] = largest;
         }
         __syncthreads();
-        r.s = r.t = 0.f;
-        r.peak = kNone;
+        r.s = r.t = largest = 0.f;
 #pragma unroll
         for (int w = 0; w < T / 64; ++w) {
             r.s += waves[1][w];
             r.t += waves[2][w];
+            largest += waves[3][w];
         }
+        r.s += largest - 1.f;
+        r.peak = r.max;
     }
     const bool nothing = r.max == -INFINITY && r.s == 0.f, bad = !(r.s == r.s) || r.max == INFINITY;
     constexpr float kLn2 = 0.693147180559945309f;
@@ -459,7 +474,7 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
     const auto logp = [&](float x) {
         if (bad) return __uint_as_float(0x7fc00000u);
         if (nothing || x == -INFINITY) return -INFINITY;
-        return fmaf(x - r.max, a.scale, most);
+        return 2.f * fmaf(0.5f * x - 0.5f * r.max, a.scale, 0.5f * most);      // (a difference may be past all numbers, its product not)
     };
     for (int i = threadIdx.x; i < a.n_tokens; i += T) {
         const given g = i < T ? first : given_of<F32>(a, v, row, i);
@@ -529,7 +544,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
         if (__any(fmaf(most, a.k, r.down) > kSlack)) {
             const float now = wave_max(most);
             take_peak(r, a.k);
-            move_to(r, -(now * a.k));
+            move_to(r, -scaled(now, a.k));
             if (most == now) {
                 r.peak = now;
                 bool found = false;

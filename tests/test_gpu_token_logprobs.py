@@ -314,3 +314,66 @@ def test_rewards_of_candidates(essa, ctx):
     a = orc.token_logprobs_limits(x)[0].max()
     assert np.abs(host(F) - want).max() <= a + 2.0 ** -20 * np.abs(lp).max()
     assert np.array_equal(order.cpu().numpy(), np.argsort(-host(F), kind="stable"))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R", [4, 530])
+@pytest.mark.parametrize("scale", [2.0 ** -120, 1e-12, 1e6, 1e30, 1e36])
+def test_extreme_scales(essa, ctx, dtype, R, scale):
+    """From rows that are all but flat to rows whose values, times the scale, single precision does not hold."""
+    x, view = _logits(R, 3001, dtype, 35)
+    _check(essa, ctx, x, view, _tokens(R, 3001, 2, 36), 5, scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R,V", [(26, 900), (13, 30000), (533, 600), (520, 6000), (208, 30000)])
+@pytest.mark.parametrize("scale", [1.0, 0.3])
+def test_values_that_stand_for_nothing(essa, ctx, dtype, R, V, scale):
+    """Large numbers in forbidden places, in front of the logits that count, among them, everywhere; logits of every size, where single precision's steps of scaled
+    logits are below one, a few, and far more."""
+    def edit(x):
+        g = np.random.default_rng(37)
+        half = g.random(V) < 0.5
+        for i, fill in enumerate((-1e30, -1e20, -1e9, -1e5, -6e7)):
+            x[i::13, :3 * V // 4] = fill
+            x[i + 5::13, half] = fill
+        x[1::13] = -1e30
+        x[1::13, V - 2] = 3.0
+        x[5::13] = -1e30
+        x[6::13] = 1e30
+        x[6::13, half] = 9.9e29
+        for i, shift in ((10, 1e9), (11, 4.65e7), (12, -4.65e7)):
+            x[i::13] = shift + 20 * x[i::13]
+    x, view = _logits(R, V, dtype, 38, edit=edit)
+    tokens = np.concatenate([_tokens(R, V, 3, 39), np.full((R, 1), V - 2)], 1)
+    _check(essa, ctx, x, view, tokens, 9, scale)
+    _check(essa, ctx, -x, view.mul_(-1), tokens, 9, scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("R", [3, 520])
+def test_small_scales_of_large_logits(essa, ctx, dtype, R):
+    """Differences of logits that are past all numbers, but not so times the scale."""
+    def edit(x):
+        x[:] = np.linspace(-1, 1, x.shape[1]) * float(torch.finfo(dtype).max)
+    x, view = _logits(R, 2000, dtype, 40, edit=edit)
+    _check(essa, ctx, x, view, _tokens(R, 2000, 4, 41), 6, 2.0 ** -126)
+    _check(essa, ctx, x, view, _tokens(R, 2000, 4, 41), 6, 0.25)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_any_call(essa, ctx, seed):
+    """Sizes, strides, scales, forbidden tokens and outputs as they come."""
+    g = np.random.default_rng(2000 + seed)
+    V = int(np.exp(g.uniform(0, np.log(200000 if seed % 3 else 3000))))
+    R = int(min(np.exp(g.uniform(0, np.log(1200))), 1 + 1.5e6 // V))
+    share = float(g.choice([0.0, g.uniform(0, 1), 0.999]))
+
+    def edit(x):
+        x[g.random(x.shape) < share] = -np.inf
+        if seed % 5 == 0:
+            x[:] = np.round(x)                                 # many equal ones
+    x, view = _logits(R, V, DTYPES[seed % 2], seed, spread=float(g.choice([0.1, 2, 30])), edit=edit, pad=int(g.choice([0, g.integers(1, 20)])), shift=int(g.integers(0, 9)))
+    n_top = int(g.choice([0, g.integers(1, 65)]))
+    tokens = g.integers(-1, V + 1, (R, int(g.integers(1, 9)))) if g.random() < 0.8 or not n_top else None
+    _check(essa, ctx, x, view, tokens, n_top, float(g.choice([1.0, g.uniform(0.2, 3)])), entropy=bool(g.random() < 0.7))
