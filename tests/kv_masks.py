@@ -66,7 +66,7 @@ def check_masked(got, q, cache, seqs, rows, scale, masks, layer=0, out_dtype=tor
         assert (y[~seen.any(1)] == 0).all()
         if not exact32 and np.isfinite(K).all() and np.isfinite(V).all():
             (k, _), (v, size), g = levels(cache.K[layer][s]), levels(cache.V[layer][s]), q.shape[1] // K.shape[1]
-            for j in sorted({0, n // 3, n - 1}):
+            for j in sorted({0, n // 3, n - 1} if n else ()):
                 for h in range(q.shape[1]):
                     if seen[j].any() and np.isfinite(qq[j, h]).all():
                         ref, limit = limits(qq[j, h].astype(np.float64), k[:, h // g], v[:, h // g], size[:, h // g], seen[j], scale)

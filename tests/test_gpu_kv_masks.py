@@ -261,3 +261,90 @@ def test_recorded(essa):
         graph.close()
         c.kv.close()
         ctx.close()
+
+
+def test_two_recorded_calls_of_one_context(essa):
+    """Attention of a tree and log probabilities, recorded one by one, share the context's scratch: replayed in turn, with calls that are not recorded between."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        ctx = essa.Context(0, stream)
+        g = np.random.default_rng(61)
+        c = Cache(essa, ctx, [9000, 700], 2, 128, 64, dtype=torch.bfloat16, seed=62)
+        rows, hq = [9, 30], 6
+        qd = values((39, hq, 128), g, torch.bfloat16)[1]
+        tree, batch = tree_words([ancestors(random_tree(g, n)) for n in rows], 1), essa.KvBatch(i32([0, 1]), starts(rows), 39)
+        logits = values((3, 50001), g, torch.bfloat16)[1]
+        tokens = torch.from_numpy(g.integers(0, 50001, (3, 2))).int().cuda()
+        Y, Z = torch.empty_like(qd), torch.empty_like(qd)
+        logp, h, ids, top = torch.empty(3, 2, device="cuda"), torch.empty(3, device="cuda"), torch.empty(3, 7, device="cuda", dtype=torch.int32), torch.empty(3, 7, device="cuda")
+        calls = [lambda: essa.essa_kv_attention(ctx, c.kv, 0, qd, Y, batch, 0.1, tree=tree),
+                 lambda: essa.essa_token_logprobs(ctx, logits, tokens, logp, 1.0, h, ids, top),
+                 lambda: essa.essa_kv_attention(ctx, c.kv, 0, qd, Z, batch, 0.1, 4000, sinks=2000)]
+        outs = [[Y], [logp, h, ids, top], [Z]]
+        for call in calls:
+            call()
+        torch.cuda.synchronize()
+        want = [[o.clone() for o in out] for out in outs]
+        assert torch.isfinite(want[0][0]).all() and not torch.equal(want[0][0], want[2][0])
+        graphs = []
+        for call in calls:
+            ctx.graph_begin()
+            call()
+            graphs.append(ctx.graph_end())
+        for turn in range(4):
+            for out in outs:
+                for o in out:
+                    o.fill_(5)
+            for i in ((0, 1, 2), (2, 1, 0), (1, 0, 2), (0, 2, 1))[turn]:
+                graphs[i].launch()
+                if turn & 1:
+                    calls[(i + turn) % 3]()
+            torch.cuda.synchronize()
+            for out, w in zip(outs, want):
+                assert all(torch.equal(a, b) for a, b in zip(out, w))
+        for graph in graphs:
+            graph.close()
+        c.kv.close()
+        ctx.close()
+
+
+def test_a_word_a_row(essa, ctx):
+    """tree [R] is tree [R, 1]."""
+    g = np.random.default_rng(63)
+    c = Cache(essa, ctx, [90, 40], 2, 64, 32, dtype=torch.float32, seed=64)
+    rows = [20, 11]
+    qd = values((31, 4, 64), g, torch.float32)[1]
+    tree, batch, out = tree_words([ancestors(random_tree(g, n)) for n in rows], 1), essa.KvBatch(i32([0, 1]), starts(rows), 31), [torch.empty_like(qd) for _ in range(2)]
+    essa.essa_kv_attention(ctx, c.kv, 0, qd, out[0], batch, 0.1, tree=tree)
+    essa.essa_kv_attention(ctx, c.kv, 0, qd, out[1], batch, 0.1, tree=tree.view(-1))
+    assert torch.equal(out[0], out[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_scores_of_a_million(essa, ctx, dtype):
+    """Exponents up to 2^21 have steps of a quarter; still every row's weights are of one token or a few, and none of them overflows."""
+    lens, rows = [900, 300, 40], [300, 9, 30]
+    c = Cache(essa, ctx, lens, 2, 128, 64, dtype=dtype, seed=65)
+    for per in (rows, [20, 9, 3], None):
+        y, _ = _run(essa, ctx, c, [0, 1, 2], per, 4, dtype, 100, 8, q_scale=2e5)
+        assert np.isfinite(y).all() and (np.abs(y).max(-1) > 0.1).all()
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_any_call(essa, ctx, seed):
+    """Lengths, rows, heads, pages, windows, sinks and trees as they come."""
+    g = np.random.default_rng(1000 + seed)
+    hkv, D, dtype = int(g.integers(1, 4)), int(g.choice([64, 128])), DTYPES[seed % 2]
+    n, page = int(g.integers(1, 20)), int(g.choice([32, 64, 256]))
+    lens = [int(x) for x in np.exp(g.uniform(0, np.log(1500), n))]
+    rows = None if seed % 4 == 3 else [int(min(g.integers(0, g.choice([4, 40, 400])), length + 2)) for length in lens]
+    window, sinks = int(g.choice([0, g.integers(1, 10), g.integers(1, 900)])), int(g.choice([0, g.integers(1, 10), g.integers(1, 900)]))
+    c = Cache(essa, ctx, lens, hkv, D, page, dtype=dtype, seed=seed)
+    seqs = [int(x) if g.random() < 0.95 else -1 for x in g.permutation(n)]
+    per = [1] * n if rows is None else [rows[s] if s >= 0 else int(g.integers(0, 5)) for s in seqs]
+    if sum(per) == 0:
+        per[0] = 1
+    trees, words = None, 0
+    if g.random() < 0.6 or not (window or sinks):
+        trees, words = [ancestors(random_tree(g, k)) if k else np.zeros((0, 0), bool) for k in per], int(g.integers(1, 8))
+    _run(essa, ctx, c, seqs, None if rows is None else per, hkv * int(g.integers(1, 9)), dtype, window, sinks, trees, words, fill=int(g.integers(0, 2)), out=torch.float32 if g.random() < 0.3 else None)
