@@ -178,7 +178,8 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[4][W]) {
 // The limit is the n_top-th largest of the largest of 64 or 256 shares of the segments (upper half of the bits: a little less): few numbers instead of
 // thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
 // segments themselves are found, bit by bit.  Where too many of their values reach the limit, a higher one comes from the largest of every thread's share of
-// those; where still too many do, they are taken one after another.
+// those (of a row of one wave: of four of every thread's); where still too many do, they are taken one after another. Rows of fewer segments than n_top take such a limit
+// at once: 16000 rows of 500 with 5 34 us, but 494 with all values put in order.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSegments = 256, kCandidates = 512;
 template <int T>
@@ -365,16 +366,18 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
         __syncthreads();
         return l.found;
     };
-    int found = limit || chosen * kLogprobSegment <= kCandidates ? collect() : kCandidates + 1;
+    int found = limit ? collect() : kCandidates + 1;
     if (found > kCandidates) {
-        uint32_t mine = 0;
+        constexpr int SHARES = T == 64 ? 4 : 1;                // of a thread
+        uint32_t mine[SHARES] = {};
         each_load([&](const unsigned long long (&key)[PER]) {
 #pragma unroll
-            for (int k = 0; k < PER; ++k) mine = max(mine, (uint32_t)(key[k] >> 32));
+            for (int k = 0; k < PER; ++k) mine[k % SHARES] = max(mine[k % SHARES], (uint32_t)(key[k] >> 32));
         });
         __syncthreads();                                       // everybody has the count
         if (threadIdx.x == 0) l.found = 0;
-        limit = max(limit, limit_of_threads<T>(mine, n_top, l));
+        if constexpr (T == 64) limit = max(limit, limit_of(mine, n_top));
+        else limit = max(limit, limit_of_threads<T>(mine[0], n_top, l));
         found = collect();
     }
     if (found <= kCandidates) {
