@@ -178,8 +178,8 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[4][W]) {
 // The limit is the n_top-th largest of the largest of 64 or 256 shares of the segments (upper half of the bits: a little less): few numbers instead of
 // thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
 // segments themselves are found, bit by bit.  Where too many of their values reach the limit, a higher one comes from the largest of every thread's share of
-// those (of a row of one wave: of four of every thread's); where still too many do, they are taken one after another. Rows of fewer segments than n_top take such a limit
-// at once: 16000 rows of 500 with 5 34 us, but 494 with all values put in order.
+// those (of a row of one wave: of four of every thread's); where still too many do, they are taken one after another. Rows of few segments take such a limit
+// at once: 16000 rows of 500 with 5 33 us, but 494 with all values put in order.
 // ---------------------------------------------------------------------------------------------
 constexpr int kSegments = 256, kCandidates = 512;
 template <int T>
@@ -308,7 +308,7 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     for (int at = threadIdx.x + HOLD * T; at < segments; at += T) best = fmaxf(best, seg[at]);
     if (threadIdx.x == 0) l.segments = l.found = 0;
     uint32_t limit = limit_of_threads<T>((int)threadIdx.x < segments ? ordered(best) : 0u, n_top, l);
-    if (segments < n_top) limit = 0;                           // a largest of each is not enough
+    if (8 * ((v.n + kLogprobSegment - 1) / kLogprobSegment) < 9 * n_top) limit = 0;            // a largest of each is not enough, or says next to nothing
     for (int base = 0; base < segments; base += HOLD * T) {
         bool in[HOLD];
         int place[HOLD];
@@ -330,38 +330,38 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
         chosen = n_top;
     }
     // their values
-    const auto key_of = [&](int at, float x) -> unsigned long long {           // of value `at` of the row; 0: none
-        const uint32_t key = ordered(x);
-        return at >= v.skip && at < v.n && x > -INFINITY && key >= limit ? (unsigned long long)key << 32 | (0xffffffffu - (uint32_t)(at - v.skip)) : 0;
-    };
-    const auto value_of = [](unsigned long long key) {
-        const uint32_t b = (uint32_t)(key >> 32);
-        return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
-    };
-    const auto each_load = [&](auto use) {                     // use(keys of the 16 bytes): whole waves
+    const auto key_of = [&](int at, float x) { return (unsigned long long)ordered(x) << 32 | (0xffffffffu - (uint32_t)(at - v.skip)); };
+    const auto value_of = [](uint32_t b) { return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b); };
+    const auto least_of = [&](uint32_t limit) { return limit <= ordered(-3.402823466e38f) ? -3.402823466e38f : value_of(limit); };
+    const auto each_load = [&](auto use) {                     // use(the values of 16 bytes, -inf where there is none; the first one's place): whole waves
         for (int i = threadIdx.x; i < ((chosen * LOADS + 63) & ~63); i += T) {
             const bool real = i < chosen * LOADS;
             const int first = l.list[real ? i / LOADS : 0] * kLogprobSegment + i % LOADS * PER;
             const u32x4 w = *(const u32x4*)(v.at + (size_t)min(first, (v.n - 1) & ~(PER - 1)) * (F32 ? 4 : 2));
-            unsigned long long key[PER];
+            float x[PER];
 #pragma unroll
-            for (int k = 0; k < PER; ++k) {
-                const float x = __uint_as_float(F32 ? w[k & 3] : k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
-                key[k] = real ? key_of(first + k, x) : 0;
-            }
-            use(key);
+            for (int k = 0; k < PER; ++k) x[k] = __uint_as_float(F32 ? w[k & 3] : k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+            if (!real || first < v.skip || first + PER > v.n)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) x[k] = real && first + k >= v.skip && first + k < v.n ? x[k] : -INFINITY;
+            use(x, first);
         }
     };
     const auto collect = [&] {
-        each_load([&](const unsigned long long (&key)[PER]) {
-            bool in[PER];
-            int place[PER];
+        const float least = least_of(limit);
+        each_load([&](const float (&x)[PER], int first) {
+            int in = 0;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) in[k] = key[k] != 0;
-            places<PER>(&l.found, in, place);
+            for (int k = 0; k < PER; ++k) in |= x[k] >= least ? 1 << k : 0;
+            if (in) {                                          // a few lanes of a wave's
+                int place = atomicAdd(&l.found, __popc(in));
 #pragma unroll
-            for (int k = 0; k < PER; ++k)
-                if (in[k] && place[k] < kCandidates) l.keys[place[k]] = key[k];
+                for (int k = 0; k < PER; ++k)
+                    if (in >> k & 1) {
+                        if (place < kCandidates) l.keys[place] = key_of(first + k, x[k]);
+                        ++place;
+                    }
+            }
         });
         __syncthreads();
         return l.found;
@@ -369,11 +369,16 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     int found = limit ? collect() : kCandidates + 1;
     if (found > kCandidates) {
         constexpr int SHARES = T == 64 ? 4 : 1;                // of a thread
-        uint32_t mine[SHARES] = {};
-        each_load([&](const unsigned long long (&key)[PER]) {
+        float most[SHARES];
+        uint32_t mine[SHARES];
 #pragma unroll
-            for (int k = 0; k < PER; ++k) mine[k % SHARES] = max(mine[k % SHARES], (uint32_t)(key[k] >> 32));
+        for (int i = 0; i < SHARES; ++i) most[i] = -INFINITY;
+        each_load([&](const float (&x)[PER], int) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) most[k % SHARES] = fmaxf(most[k % SHARES], x[k]);
         });
+#pragma unroll
+        for (int i = 0; i < SHARES; ++i) mine[i] = most[i] > -INFINITY ? ordered(most[i]) : 0u;
         __syncthreads();                                       // everybody has the count
         if (threadIdx.x == 0) l.found = 0;
         if constexpr (T == 64) limit = max(limit, limit_of(mine, n_top));
@@ -386,7 +391,7 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
             int rank = 0;
 #pragma unroll 8
             for (int o = 0; o < found; ++o) rank += l.keys[o] > key;
-            if (rank < n_top) put(rank, (int)(0xffffffffu - (uint32_t)key), value_of(key));
+            if (rank < n_top) put(rank, (int)(0xffffffffu - (uint32_t)key), value_of((uint32_t)(key >> 32)));
         }
         for (int i = found + threadIdx.x; i < n_top; i += T) put(i, -1, -INFINITY);
         return;
@@ -394,9 +399,12 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     unsigned long long last = ~0ull;
     for (int rank = 0; rank < n_top; ++rank) {
         unsigned long long most = 0;
-        each_load([&](const unsigned long long (&key)[PER]) {
+        each_load([&](const float (&x)[PER], int first) {
 #pragma unroll
-            for (int k = 0; k < PER; ++k) most = key[k] < last && key[k] > most ? key[k] : most;
+            for (int k = 0; k < PER; ++k) {
+                const unsigned long long key = x[k] > -INFINITY ? key_of(first + k, x[k]) : 0;
+                most = key < last && key > most ? key : most;
+            }
         });
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
@@ -408,7 +416,7 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) most = l.most[w] > most ? l.most[w] : most;
         __syncthreads();
-        if (threadIdx.x == 0) put(rank, most ? (int)(0xffffffffu - (uint32_t)most) : -1, most ? value_of(most) : -INFINITY);
+        if (threadIdx.x == 0) put(rank, most ? (int)(0xffffffffu - (uint32_t)most) : -1, most ? value_of((uint32_t)(most >> 32)) : -INFINITY);
         last = most;
     }
 }
