@@ -297,7 +297,7 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     constexpr int WAVES = T / 64, PER = F32 ? 4 : 8, LOADS = kLogprobSegment / PER;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     // segments
-    constexpr int HOLD = T == 64 ? 1 : 1536 / T;               // of a thread, as many as its vocabularies have, or nearly
+    constexpr int HOLD = T == 64 ? 2 : 1536 / T;               // of a thread, as many as its vocabularies have, or nearly
     float held[HOLD], best = -INFINITY;
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
@@ -307,7 +307,13 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     }
     for (int at = threadIdx.x + HOLD * T; at < segments; at += T) best = fmaxf(best, seg[at]);
     if (threadIdx.x == 0) l.segments = l.found = 0;
-    uint32_t limit = limit_of_threads<T>((int)threadIdx.x < segments ? ordered(best) : 0u, n_top, l);
+    uint32_t limit;
+    if (T == 64 && n_top > 32) {                               // every one of them
+        uint32_t each[HOLD];
+#pragma unroll
+        for (int i = 0; i < HOLD; ++i) each[i] = (int)threadIdx.x + i * T < segments ? ordered(held[i]) : 0u;
+        limit = limit_of(each, n_top);
+    } else limit = limit_of_threads<T>((int)threadIdx.x < segments ? ordered(best) : 0u, n_top, l);
     if (8 * ((v.n + kLogprobSegment - 1) / kLogprobSegment) < 9 * n_top) limit = 0;            // a largest of each is not enough, or says next to nothing
     for (int base = 0; base < segments; base += HOLD * T) {
         bool in[HOLD];
@@ -637,7 +643,8 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
 namespace essa_k {
 
 static int loads_of(int V, int x_dtype) { return (V + (x_dtype == ESSA_F32 ? 3 : 7) + kLoad - 1) / kLoad; }
-// Threads of a workgroup, and workgroups a row.  One wave does a row of few loads (8192 rows of 1000 below); where rows are about as many as CUs one large
+// Threads of a workgroup, and workgroups a row.  One wave does a row of few loads, or of 32 in bf16 where rows are many (16000 rows of 8000 with
+// 5 of them 59 us, 88 with four waves a row; without them 44, 56; in fp32 104 and 112, 93 and 88); where rows are about as many as CUs one large
 // workgroup each spares the parts' joining; fewer rows are shared, so that the chip has two workgroups a CU; many rows of a large vocabulary
 // run a little better with eight waves than with four.  us with 256 threads and up to 1024 workgroups, 512 and 512, 1024 and one a row: 256 rows of 152064 with 20 of
 // them 26.5, 24.7, 22.7; 160 with 5 19.2, 18.5, 19.9; 64 with 5 13.1, 13.1, 13.4; 400 with 8 37.0, 33.4, 39.5, but 300 with 5 28.2, 32.5, 37.5; 2048 with 20
@@ -647,7 +654,7 @@ struct shape {
 };
 static shape shape_of(int R, int V, int x_dtype) {
     const int loads = loads_of(V, x_dtype);
-    if (loads <= 8) return {64, 1};
+    if (loads <= 8 || (R >= 2048 && x_dtype == ESSA_BF16 && loads <= 32)) return {64, 1};
     if (R >= kLogprobSplitRows) return {loads >= 128 ? 512 : 256, 1};
     if (R > 192 && R <= 256) return {1024, 1};
     return {512, std::max(1, std::min({256, loads / 8, 512 / R}))};

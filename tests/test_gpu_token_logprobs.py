@@ -361,6 +361,22 @@ def test_small_scales_of_large_logits(essa, ctx, dtype, R):
     _check(essa, ctx, x, view, _tokens(R, 2000, 4, 41), 6, 0.25)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,top", [(4100, 5), (8100, 64), (16300, 40), (16300, 64), (16383, 3), (900, 64)])
+def test_many_rows_of_middle_size(essa, ctx, dtype, V, top):
+    """One wave a row; equal, sorted, forbidden and all but certain logits among them."""
+    def edit(x):
+        g = np.random.default_rng(42)
+        x[::7] = np.round(x[::7])
+        x[1::70] = np.sort(x[1::70])
+        x[2::70] = -np.sort(-x[2::70])
+        x[3::70] = 1.0
+        x[4::7][g.random(x[4::7].shape) < 0.997] = -np.inf
+        x[5::7, 77] = 40.0
+    x, view = _logits(2050, V, dtype, 43, edit=edit, pad=3)
+    _check(essa, ctx, x, view, _tokens(2050, V, 1, 44), top)
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_any_call(essa, ctx, seed):
     """Sizes, strides, scales, forbidden tokens and outputs as they come."""
