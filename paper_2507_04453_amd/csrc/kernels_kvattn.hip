@@ -106,6 +106,8 @@ constexpr int kLittle = 8192;
 // Masks: calls of little work in units of kNarrow columns, where every wave takes a block in four, instead of 64, where each takes all of them: more units to
 // share, and a quarter of the steps one after another.  Trees of 26 rows (28 heads on 4), us with 64 and with 16: one of 500 tokens (of 16 rows) 28, 14; 8 of 1000 44, 23;
 // 16 of 1000 46, 30; fp32 (8 heads of 64, 63 rows) one of 600 43, 17, but 64 of them, 12800 long, 74 and 90.
+// Where there would be more of them than workgroups (fp32: than twice as many) a unit's start costs more than that gives: 90 trees of 2 rows (128 heads on 8) 16 and 28, 25 of
+// 28 (48 on 3 of 64) 12 and 20, 95 of 24 (8 on 4 of 64) 17 and 23, 3 of 143 behind a window of 19 (32 on 4) 22 and 26; fp32 one of 147 (128 on 8, 1184 units) 55 and 49.
 constexpr int kNarrow = 16;
 // Masks: where every workgroup can have one unit's part alone it does not begin another's behind it, which costs it about kAligned blocks more.
 constexpr int kAligned = 16;
@@ -154,18 +156,25 @@ __device__ attn_list make_list(const attn_args& a, void* lds) {                /
     const int n = a.rows.n, per = (n + 255) / 256, lo = min((int)threadIdx.x * per, n), hi = min(lo + per, n);
     attn_list l{(int*)((int2*)lds + (OWN_ROWS ? 2 * n : n)), (int2*)lds, OWN_ROWS ? (int2*)lds + n : nullptr, 0, 0, false, kColumns, false};
     if (OWN_ROWS && ((!F32 && a.tiles) || MASK)) {                         // every workgroup finds the same
-        int work = 0;
+        int work = 0, narrow = 0;
         for (int b = lo; b < hi; ++b) {
             const kv_entry e = kv_entry_of(a.v, a.rows, b);
             const entry_span s = span_of<MASK>(a, e.len, e.rows);
-            if (s.n) work += (int)min((long long)s.groups * a.v.heads * (s.n + kUnitCost), (long long)kLittle + 1);
+            if (s.n) {
+                work += (int)min((long long)s.groups * a.v.heads * (s.n + kUnitCost), (long long)kLittle + 1);
+                if (MASK) narrow += (int)min((long long)span_of<MASK>(a, e.len, e.rows, kNarrow).groups * a.v.heads, (long long)kLittle);
+            }
         }
         work = wave_scan(work, [](int x, int y) { return x + y; });
-        if ((threadIdx.x & 63) == 63) waves[0][threadIdx.x / 64] = work;
+        if (MASK) narrow = wave_scan(narrow, [](int x, int y) { return x + y; });
+        if ((threadIdx.x & 63) == 63) {
+            waves[0][threadIdx.x / 64] = work;
+            if (MASK) waves[1][threadIdx.x / 64] = narrow;
+        }
         lds_barrier();
         work = uniform(waves[0][0] + waves[0][1] + waves[0][2] + waves[0][3]);
         l.prompts = !F32 && a.tiles && work > kLittle;
-        if (MASK && work <= kLittle) l.width = kNarrow;
+        if (MASK && work <= kLittle && uniform(waves[1][0] + waves[1][1] + waves[1][2] + waves[1][3]) <= (F32 ? 2 : 1) * (int)gridDim.x) l.width = kNarrow;
         lds_barrier();
     }
     int length = 0, units = 0, longest = 0, rows = 0;          // (16 entries a thread at most: their rows are an int)
