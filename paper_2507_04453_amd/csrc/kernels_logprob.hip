@@ -224,24 +224,6 @@ __device__ uint32_t limit_of_threads(uint32_t key, int want, top_lds<T>& l) {
     const uint32_t one[1] = {mine[0]};
     return limit_of(one, want);
 }
-// places[i] for those of a lane's N numbers that are `in`: one atomic a wave
-template <int N>
-__device__ __forceinline__ void places(int* count, const bool (&in)[N], int (&place)[N]) {
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const unsigned long long has = __ballot(in[i]);
-        place[i] = total + __popcll(has & ((1ull << lane) - 1));
-        total += __popcll(has);
-    }
-    if (total == 0) return;
-    int first = 0;
-    if (lane == 0) first = atomicAdd(count, total);
-    first = __builtin_amdgcn_readfirstlane(first);
-#pragma unroll
-    for (int i = 0; i < N; ++i) place[i] += first;
-}
 // The `want` first segments into l.list: returns the limit that parts them from the rest.
 template <bool F32, int T>
 __device__ uint32_t first_segments(const float* seg, int segments, int want, top_lds<T>& l) {
@@ -297,7 +279,7 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
     constexpr int WAVES = T / 64, PER = F32 ? 4 : 8, LOADS = kLogprobSegment / PER;
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
     // segments
-    constexpr int HOLD = T == 64 ? 2 : 1536 / T;               // of a thread, as many as its vocabularies have, or nearly
+    constexpr int HOLD = T == 64 || T == 1024 ? 2 : 1536 / T;               // of a thread, as many as its vocabularies have, or nearly
     float held[HOLD], best = -INFINITY;
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
@@ -313,24 +295,31 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
 #pragma unroll
         for (int i = 0; i < HOLD; ++i) each[i] = (int)threadIdx.x + i * T < segments ? ordered(held[i]) : 0u;
         limit = limit_of(each, n_top);
+        __syncthreads();                                       // the counts are 0
     } else limit = limit_of_threads<T>((int)threadIdx.x < segments ? ordered(best) : 0u, n_top, l);
     if (8 * ((v.n + kLogprobSegment - 1) / kLogprobSegment) < 9 * n_top) limit = 0;            // a largest of each is not enough, or says next to nothing
-    for (int base = 0; base < segments; base += HOLD * T) {
-        bool in[HOLD];
-        int place[HOLD];
+    const bool all = limit == 0 && segments <= kSegments;
+    for (int at = threadIdx.x; all && at < segments; at += T) l.list[at] = at;
+    for (int base = 0; !all && base < segments; base += HOLD * T) {
+        int in = 0;
 #pragma unroll
         for (int i = 0; i < HOLD; ++i) {
             const int at = base + (int)threadIdx.x + i * T;
             const float x = base == 0 ? held[i] : seg[min(at, segments - 1)];
-            in[i] = at < segments && ordered(x) >= limit;
+            in |= at < segments && ordered(x) >= limit ? 1 << i : 0;
         }
-        places<HOLD>(&l.segments, in, place);
+        if (in) {                                              // a few lanes' of a wave: an atomic each
+            int place = atomicAdd(&l.segments, __popc(in));
 #pragma unroll
-        for (int i = 0; i < HOLD; ++i)
-            if (in[i] && place[i] < kSegments) l.list[place[i]] = base + threadIdx.x + i * T;
+            for (int i = 0; i < HOLD; ++i)
+                if (in >> i & 1) {
+                    if (place < kSegments) l.list[place] = base + threadIdx.x + i * T;
+                    ++place;
+                }
+        }
     }
     __syncthreads();
-    int chosen = l.segments;
+    int chosen = all ? segments : l.segments;
     if (chosen > kSegments) {
         limit = first_segments<F32, T>(seg, segments, n_top, l);
         chosen = n_top;
@@ -387,8 +376,10 @@ __device__ void find_top(const row_view<F32>& v, const float* seg, int segments,
         for (int i = 0; i < SHARES; ++i) mine[i] = most[i] > -INFINITY ? ordered(most[i]) : 0u;
         __syncthreads();                                       // everybody has the count
         if (threadIdx.x == 0) l.found = 0;
-        if constexpr (T == 64) limit = max(limit, limit_of(mine, n_top));
-        else limit = max(limit, limit_of_threads<T>(mine[0], n_top, l));
+        if constexpr (T == 64) {
+            limit = max(limit, limit_of(mine, n_top));
+            __syncthreads();
+        } else limit = max(limit, limit_of_threads<T>(mine[0], n_top, l));
         found = collect();
     }
     if (found <= kCandidates) {
