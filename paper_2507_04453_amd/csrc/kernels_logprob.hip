@@ -508,9 +508,9 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
 
 // A row is one workgroup's, or (few rows) several's: then each leaves its sums and its segments' largest values, and the last to come finishes the row.
 // Logits are read once, four loads of a wave on their way.  8192 rows of 152064 in bf16: 421 us, 5.9 TB/s, which is what reading reaches, with the vector
-// ALU working 94 % of the time (a logit takes it eight instructions, the exponential among them).  256 rows with the 20 most probable of each: 21.6 us, 3.6 TB/s,
-// 16.7 without them: what finding them takes is a chain of short steps (limit 1400 cycles, list 2300, reading the segments again 3700, order 1500), of which
-// calls of many rows hide all but 4 %.  One row: 8.9 us, 6.7 without the most probable, most of that the call's.
+// ALU working 91 % of the time (a logit takes it eight instructions, the exponential among them).  256 rows with the 20 most probable of each: 21.3 us, 3.6 TB/s,
+// 16.7 without them: what finding them takes is a chain of short steps (the limit, the list, reading the segments again, their order), of which
+// calls of many rows hide all but 4 %.  One row: 8.6 us, 6.7 without the most probable, most of that the call's.
 template <bool F32, bool TOP, int T>
 __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
     extern __shared__ float seg[];                             // [segments of this part], then of the row
