@@ -330,6 +330,37 @@ def test_scores_of_a_million(essa, ctx, dtype):
         assert np.isfinite(y).all() and (np.abs(y).max(-1) > 0.1).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1e-30, 3.0])
+def test_scales(essa, ctx, dtype, scale):
+    g = np.random.default_rng(66)
+    lens, rows = [300, 90, 500, 64], [70, 9, 200, 64]
+    c = Cache(essa, ctx, lens, 2, 64, 32, dtype=dtype, seed=67)
+    trees = [ancestors(random_tree(g, n)) for n in rows]
+    for many, per in ((4, rows), (2, [5, 3])):
+        _run(essa, ctx, c, list(range(many)), per, 8, dtype, 40, 7, [t[:n, :n] for t, n in zip(trees, per)], 4, scale=scale)
+        _run(essa, ctx, c, list(range(many)), per, 8, dtype, 40, 7, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [[3, 9, 1], [200, 150, 300]])
+def test_rows_behind_the_last_entry(essa, ctx, dtype, rows):
+    """They are nobody's, and stay as they were; so does memory around Y."""
+    n, R = sum(rows), sum(rows) + 21
+    c = Cache(essa, ctx, [500, 150, 900], 4, 128, 64, dtype=dtype, seed=68)
+    Q = torch.randn(R, 28, 128, device="cuda").to(dtype)
+    around = torch.full((R + 4, 28 * 128 + 8), 5.0, device="cuda", dtype=dtype)
+    Y = around[2:R + 2, 8:]                                    # rows apart, their beginning on 16 bytes
+    tree = torch.full((R, 2), -1, device="cuda")
+    for kw in ({"sinks": 3}, {"tree": tree}, {"sinks": 70, "tree": tree}):
+        around.fill_(5.0)
+        essa.essa_kv_attention(ctx, c.kv, 0, Q, Y, essa.KvBatch(i32([0, 1, 2]), starts(rows), R), 0.1, 60, **kw)
+        y = around.clone()
+        assert torch.isfinite(y).all() and not (y[2:n + 2, 8:] == 5).all(1).any()
+        y[2:n + 2, 8:] = 5.0
+        assert (y == 5).all()
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_any_call(essa, ctx, seed):
     """Lengths, rows, heads, pages, windows, sinks and trees as they come."""
