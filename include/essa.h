@@ -496,7 +496,8 @@ essa_status essa_kv_read(essa_ctx* ctx, const essa_kv* kv, int layer, void* K, i
  * weights and weights times scales are rounded to fp16 (with the largest weight at 2^13 or more and scales brought below 1, so that
  * values of any size from 1e-6 up keep its 11 bits); in calls of much work, entries with more than 64 pairs (row, query head) of a key head
  * have K, V and the weights rounded to fp16 instead, so that a row's last bits depend on what else is in the call.  fp32 Q: fp32 throughout.
- * Scores times scale lie within +-2^22: past that single precision's steps of them are whole exponents, and a row may come out as NaN.
+ * Scores are single precision, however large: where their steps are whole exponents a row is what its largest score says.  Nothing overflows (a row that does is NaN) while
+ * |Q| is below 2^112 and |Q| and the scores, as they are and times scale log2(e), below 2^127.
  * Equal calls give equal bits.
  * The first call, and one larger than all before it, may allocate scratch (ESSA_ERR_STATE while a graph is recorded or alive). */
 #define ESSA_KV_ALL 0x1u
