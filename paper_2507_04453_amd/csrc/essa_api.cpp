@@ -1032,10 +1032,15 @@ extern "C" essa_status essa_token_logprobs(essa_ctx* ctx, const void* logits, in
         if (ctx->capturing) return essa_fail(ESSA_ERR_STATE, "%s: its first call makes its counts: run it once before essa_graph_begin", who);
         void* p = nullptr;
         const size_t bytes = essa_k::kLogprobSplitRows * essa_k::kLogprobCountStep * sizeof(int32_t);
-        const hipError_t e = device_alloc(&p, bytes);
+        hipError_t e = device_alloc(&p, bytes);
         if (e != hipSuccess) return essa_fail(ESSA_ERR_OOM, "%s: hipMalloc of %zu bytes: %s", who, bytes, hipGetErrorString(e));
+        e = hipMemsetAsync(p, 0, bytes, ctx->stream);
+        if (e != hipSuccess) {                                 // counts that are not 0 would leave rows unfinished, call after call
+            (void)hipGetLastError();
+            (void)hipFree(p);
+            return essa_fail(ESSA_ERR_HIP, "%s: clearing its counts: %s", who, hipGetErrorString(e));
+        }
         ctx->counts = (int32_t*)p;
-        ESSA_HIP(hipMemsetAsync(p, 0, bytes, ctx->stream));
     }
     ESSA_TRY(essa_ws_reserve(ctx, essa_k::token_logprobs_bytes(R, V, x_dtype, n_top)));
     essa_k::logprob_args a{};
