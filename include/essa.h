@@ -511,7 +511,8 @@ essa_status essa_kv_attention(essa_ctx* ctx, const essa_kv* kv, int layer, const
  *          front of them (t < len - c), and of the rows' own tokens that of row u where bit u % 64 of tree[row * tree_words + u / 64] is set
  *          (its ancestors and itself, in a tree; what is not set it does not see, itself included, and rows past 64 tree_words nobody sees).  Bits from
  *          c on are not looked at.  With a window the row's position p is len - c and one more for every other row that it sees, and the tokens in front of the
- *          rows are seen if t > p - window or t < sinks; what is set among the rows is seen at any distance.
+ *          rows are seen if t > p - window or t < sinks; what is set among the rows is seen at any distance.  Where the window has to hold among them as well (a path longer than
+ *          it), a row's words name the last `window` rows of its path, itself among them, and the sinks: it then sees what a causal row would there.
  * tree: DEVICE uint64 [R, tree_words], 8-byte aligned, read by the call; tree_words = 0: no tree.  With neither sinks nor a tree the call gives the bits of
  * essa_kv_attention. */
 #define ESSA_KV_TREE_WORDS 16
