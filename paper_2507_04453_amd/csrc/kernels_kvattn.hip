@@ -612,10 +612,10 @@ constexpr float kTileSlack = 8.f, kTileLift = 4.f;            // prompts: weight
 constexpr float kLift = 13.f;  // weights are 2^kLift larger than they have to be: fp16's small numbers reach further down
 // Where the exponent of the running maximum is past 2^22 in size, `down` would be rounded by a quarter of an exponent and more, at 2^24 by whole ones: weights would pass
 // what fp16 holds, or all be 0.  Such a column is far: its scores are taken relative to the maximum first, which is exact for those that count, and its `down` is the
-// lift alone.  Other calls pay a scalar branch a block: one row of 256 sequences of 130 to 2100 tokens (28 heads on 4 of 128) 37.2 -> 37.4 us, prompts of up to 2000 rows
-// 558 -> 560, four of 100000 tokens 107.0 -> 107.2.
+// lift alone.  It does so where the maximum moves, which its slack has it do with every block, so that other columns pay a comparison where theirs moves.
+// A tree of 63 rows behind 1986 tokens 25.3 -> 25.5 us (26.4 with a branch of its own in every block), one row of 256 sequences behind a window 39.9 -> 40.1, one of 256
+// of 130 to 2100 tokens 37.4 -> 37.7, prompts as before.
 constexpr float kFarFrom = 4194304.f;
-__device__ __forceinline__ bool is_far(float top, float kappa) { return top > -kFar && fabsf(top * kappa) > kFarFrom; }
 constexpr int kScaleOne = 14;  // exponent field of fp16 just below 1
 
 template <int D>
@@ -674,11 +674,10 @@ struct attn_state {
     float less[NG];            // what the scores' accumulators start from
     code_masks masks;
     float kappa;               // score in units of q -> exponent of 2
-    float slack;               // kSlack in units of the score
+    float slack;               // kSlack in units of the score; -inf of a far column
     int vlo, vhi;              // tokens that the column sees
     float top;                 // running maximum, in units of the score
     float down;                // kLift - top * kappa; kLift where that is far
-    bool some_far;             // a column of the wave's is far
     float sum, mid[NG];        // this lane's tokens' share of sum p and sum p m
     f32x4 o[D / 16];           // channel 16 i + 4 (lane / 16) + r; bf16: times what the group's scales are times
     int big[NG];               // bf16: exponent field of the largest scale of values so far, kScaleOne at least; the same in every lane
@@ -739,7 +738,6 @@ struct attn_state {
         vlo = real ? (a.window > 0 ? max(pos - a.window + 1, 0) : 0) : 0;
         top = -kFar;
         down = kLift;
-        some_far = false;
         sum = real && !finite && (MASK ? sees() : vlo < vhi) ? NAN : 0.f;        // a query that is not finite: everything that follows is NaN
 #pragma unroll
         for (int gr = 0; gr < NG; ++gr) {
@@ -829,19 +827,18 @@ struct attn_state {
             const float now = fmaxf(top, quarters_max(m));
             const float f = now == top ? 1.f : __builtin_amdgcn_exp2f(fmaxf(top - now, -kFar) * kappa);
             top = now;
-            const bool far = is_far(now, kappa);
-            down = now > -kFar && !far ? fmaf(-now, kappa, kLift) : kLift;
-            some_far = __any(far);
+            down = now > -kFar ? fmaf(-now, kappa, kLift) : kLift;
+            if (const bool far = fabsf(down) > kFarFrom; __any(far)) {
+                slack = far ? -INFINITY : slack;               // and here again with every block
+                down = far ? kLift : down;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] -= far ? now : 0.f;
+            }
             sum *= f;
 #pragma unroll
             for (int gr = 0; gr < NG; ++gr) mid[gr] *= f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[i] *= f;
-        }
-        if (some_far) {
-            const float from = is_far(top, kappa) ? top : 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] -= from;
         }
         float p[8];
 #pragma unroll
@@ -1430,9 +1427,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                 }
             sum = real && !finite && (MASK ? sight.any(a, len, rows) : vlo < vhi) ? NAN : 0.f;
         }
-        const float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
+        float slack = real ? kTileSlack * __builtin_amdgcn_rcpf(kappa) : INFINITY;
         float top = -kFar, down = kTileLift;
-        bool some_far = false;                                 // a column of the wave's is far
         f32x16 o[OT];
 #pragma unroll
         for (int i = 0; i < OT; ++i)
@@ -1516,20 +1512,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void kv_attn_prompt_kernel(attn_ar
                         const float new_top = fmaxf(top, m);
                         const float f = new_top == top ? 1.f : __builtin_amdgcn_exp2f(fmaxf(top - new_top, -kFar) * kappa);
                         top = new_top;
-                        const bool far = is_far(new_top, kappa);
                         down = fmaf(-new_top, kappa, kTileLift);
-                        down = new_top > -kFar && !far ? down : kTileLift;
-                        some_far = __any(far);
+                        down = new_top > -kFar ? down : kTileLift;
+                        if (const bool far = fabsf(down) > kFarFrom; __any(far)) {
+                            slack = far ? -INFINITY : slack;   // and here again with every stage
+                            down = far ? kTileLift : down;
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                                for (int k = 0; k < 16; ++k) s[i][k] -= far ? new_top : 0.f;
+                        }
                         sum *= f;
 #pragma unroll
                         for (int i = 0; i < OT; ++i) o[i] *= f;
-                    }
-                    if (some_far) {
-                        const float from = is_far(top, kappa) ? top : 0.f;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) s[i][k] -= from;
                     }
                     const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
 #pragma unroll
