@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256) void kv_fork_tables_kernel(pages_view v, const
 // token is overwritten before it has moved.  Workgroup (b, y) looks for itself whether the entry can be served and moves its share of the heads of
 // all layers; the last of an entry's to have done so, when nobody looks at its tables any more, gives the pages behind the path back.
 // Bound by the latency of looks at tables, one behind the other, and of the two trips that a moved token makes: 64 trees of 8 to 63 rows in four layers of
-// four heads of 128 take 12.4 us, one of 9 rows in two layers 6.8, of which the bytes moved are under 1.
+// four heads of 128 take 12.8 us, one of 9 rows in two layers 6.3, of which the bytes moved are under 1.
 struct accept_entry {
     int ok;                    // the sequence, or why not
     int row0, len, base, keep, moved;   // moved: the first row of the path that is not where it was

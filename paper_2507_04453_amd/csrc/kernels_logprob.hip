@@ -175,8 +175,8 @@ __device__ void join_threads(row_sums& a, float k, float (&waves)[4][W]) {
 // The n_top largest of a row.  A segment is kLogprobSegment consecutive values, of which `seg` (LDS) holds the largest.  With segments ordered by
 // it, the earlier of equal ones first, the n_top largest values lie in the n_top first segments: a value outside of them has one in each
 // in front of it.  So a few segments are read again, and of them what is not below a limit that n_top values reach is put in order.
-// The limit is the n_top-th largest of the largest of 64 or 256 shares of the segments (upper half of the bits: a little less): few numbers instead of
-// thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
+// The limit is the n_top-th largest of the largest of 64 shares of the segments, for more than 32 of one share of every thread, of a row of one wave of the segments themselves (upper
+// half of the bits: a little less): few numbers instead of thousands, and hardly more segments than n_top reach it.  Where more do than there is room for (sorted logits, ties everywhere), the n_top first
 // segments themselves are found, bit by bit.  Where too many of their values reach the limit, a higher one comes from the largest of every thread's share of
 // those (of a row of one wave: of four of every thread's); where still too many do, they are taken one after another. Rows of few segments take such a limit
 // at once: 16000 rows of 500 with 5 33 us, but 494 with all values put in order.
@@ -508,9 +508,9 @@ __device__ void finish_row(const logprob_args& a, const row_view<F32>& v, int ro
 
 // A row is one workgroup's, or (few rows) several's: then each leaves its sums and its segments' largest values, and the last to come finishes the row.
 // Logits are read once, four loads of a wave on their way.  8192 rows of 152064 in bf16: 421 us, 5.9 TB/s, which is what reading reaches, with the vector
-// ALU working 91 % of the time (a logit takes it eight instructions, the exponential among them).  256 rows with the 20 most probable of each: 21.3 us, 3.6 TB/s,
-// 16.7 without them: what finding them takes is a chain of short steps (the limit, the list, reading the segments again, their order), of which
-// calls of many rows hide all but 4 %.  One row: 8.6 us, 6.7 without the most probable, most of that the call's.
+// ALU working 91 % of the time and more (a logit takes it eight instructions, the exponential among them).  256 rows with the 20 most probable of each: 21.5 us, 3.6 TB/s,
+// 17.1 without them: what finding them takes is a chain of short steps (the limit, the list, reading the segments again, their order), of which
+// calls of many rows hide all but 4 %.  One row, recorded: 9.1 us, 6.0 without the most probable.
 template <bool F32, bool TOP, int T>
 __global__ __launch_bounds__(T) void token_logprobs_kernel(logprob_args a) {
     extern __shared__ float seg[];                             // [segments of this part], then of the row
@@ -637,7 +637,7 @@ static int loads_of(int V, int x_dtype) { return (V + (x_dtype == ESSA_F32 ? 3 :
 // Threads of a workgroup, and workgroups a row.  One wave does a row of few loads, or of 32 in bf16 where rows are many (16000 rows of 8000 with
 // 5 of them 59 us, 88 with four waves a row; without them 44, 56; in fp32 104 and 112, 93 and 88); where rows are about as many as CUs one large
 // workgroup each spares the parts' joining; fewer rows are shared, so that the chip has two workgroups a CU; many rows of a large vocabulary
-// run a little better with eight waves than with four.  us with 256 threads and up to 1024 workgroups, 512 and 512, 1024 and one a row: 256 rows of 152064 with 20 of
+// run a little better with eight waves than with four.  From 257 to 511 rows neither side is best everywhere; one workgroup of 512 a row is not for 300 of 152064.  us with 256 threads and up to 1024 workgroups, 512 and 512, 1024 and one a row: 256 rows of 152064 with 20 of
 // them 26.5, 24.7, 22.7; 160 with 5 19.2, 18.5, 19.9; 64 with 5 13.1, 13.1, 13.4; 400 with 8 37.0, 33.4, 39.5, but 300 with 5 28.2, 32.5, 37.5; 2048 with 20
 // 127, 120, 160; 4096 of 32000 with 20 64.7, 71.7, 132.
 struct shape {
